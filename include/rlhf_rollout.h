@@ -47,7 +47,8 @@ typedef enum {
   RLHF_EUNSUPPORTED = -4  /* dtype / head_dim / size outside what the kernels are built for */
 } rlhf_status;
 
-enum { RLHF_DTYPE_FP32 = 0, RLHF_DTYPE_BF16 = 1 };
+/* RLHF_DTYPE_FP16: token statistics only (rlhf_token_stats); a model is FP32 or BF16. */
+enum { RLHF_DTYPE_FP32 = 0, RLHF_DTYPE_BF16 = 1, RLHF_DTYPE_FP16 = 2 };
 
 /* Model shape.  Architecture: pre-LayerNorm decoder with parallel residual
  * x <- x + Attn(LN1(x)) + MLP(LN2(x)), exact-erf GELU, rotary embedding on the first rotary_dims
@@ -223,6 +224,79 @@ int rlhf_ppo_loss(const float *new_logprobs, const float *old_logprobs, const fl
 int rlhf_adamw_step(float *param, const float *grad, float *exp_avg, float *exp_avg_sq, uint16_t *param_bf16,
                     uint64_t n, int32_t step, double lr, double beta1, double beta2, double eps,
                     double weight_decay, double grad_scale, void *stream);
+
+/* ---- Both ends of a policy update beside the passes of a handle's model (stateless). -------------------
+ *
+ * Token statistics: log-probabilities of given tokens, entropies and the most likely alternatives of rows of hidden
+ * states under an output matrix (paper: Preliminaries, Eq. (RL), the log-probabilities of the KL term; PPO hyperparameter
+ * table, the sampling temperature that divides the logits).  For rows t < T, with l = W h_t and z = l / temperature,
+ *   out_lse[t]      = log sum_v exp z_v
+ *   out_logprobs[t] = z_y - lse for y = targets[t]; 0 where y is not an id in [0, V) (-1: no target)
+ *   out_entropy[t]  = - sum_v p_v log p_v with p = softmax(z)
+ *   out_top_ids / out_top_logprobs [T, top_k] = the top_k entries of largest l, largest first, equal ones by lower id
+ *                     (NaN last), and their z - lse.  Required iff top_k > 0; top_k at most 64 and at most V.
+ * hidden: dev [T, d], rows ld_hidden elements apart; weight: dev [V, d], rows ld_weight apart (both >= d, bases 16-byte
+ * aligned), both float (RLHF_DTYPE_FP32), bfloat16 (RLHF_DTYPE_BF16) or IEEE half (RLHF_DTYPE_FP16): a policy's hidden
+ * states after its final LayerNorm and its embed_out.  targets: dev int32 [T]; outputs dev float (ids int32), all but the
+ * alternatives required.  V at most 262,144.  Products are summed in fp32; logits are not rounded to the inputs' type.
+ * Where d is not a multiple of 64 (32 for float) or a row is not whole 16 bytes, both matrices are copied into the
+ * workspace first (in the backward call also where V or T is not such a multiple).  Rows do not depend on each other.
+ * With top_k = 0 no logit is stored; else those of 4,096 rows at a time are, in the workspace. */
+int rlhf_token_stats_workspace_bytes(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight, int32_t dtype,
+                                     int32_t top_k, size_t *out);
+int rlhf_token_stats(const void *hidden, int64_t ld_hidden, const void *weight, int64_t ld_weight, const int32_t *targets,
+                     int32_t T, int32_t d, int32_t V, int32_t dtype, float temperature, int32_t top_k, float *out_logprobs,
+                     float *out_entropy, float *out_lse, int32_t *out_top_ids, float *out_top_logprobs, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/* Gradient of the above: from dL/dlogprob and dL/dentropy (an entropy bonus) to the two operands.  With lse and entropy
+ * as rlhf_token_stats returned them for the same inputs and temperature, p = exp(z - lse), g = d_logprobs[t] (ignored where
+ * the row has no target) and e = d_entropy[t],
+ *   dl_v = (g ([v = y] - p_v) - e p_v (log p_v + entropy)) / temperature
+ *   d_hidden [T, d] = dl W,   d_weight [V, d] = dl^T h        (contiguous, overwritten)
+ * d_entropy (and then entropy too) may be NULL.  grad_dtype: the type of both outputs, the inputs' type or RLHF_DTYPE_FP32.
+ * dl is rounded to the inputs' type for its products (relative 2^-8 for bfloat16, 2^-11 for half, whose range it is brought
+ * into by a power of two that is divided out again); sums are fp32, in a fixed order, over T too, also where T exceeds the
+ * 16,384 rows of dl that exist at a time in the workspace. */
+int rlhf_token_stats_backward_workspace_bytes(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight,
+                                              int32_t dtype, int32_t grad_dtype, size_t *out);
+int rlhf_token_stats_backward(const void *hidden, int64_t ld_hidden, const void *weight, int64_t ld_weight,
+                              const int32_t *targets, const float *lse, const float *entropy, const float *d_logprobs,
+                              const float *d_entropy, int32_t T, int32_t d, int32_t V, int32_t dtype, float temperature,
+                              int32_t grad_dtype, void *d_hidden, void *d_weight, void *workspace, size_t workspace_bytes,
+                              void *stream);
+
+/* Orthogonalisation by Newton-Schulz products, of `batch` matrices [rows, cols] one after the other in memory:
+ *   X = x / (|x|_F + eps);  ns_steps times  A = X X^T,  X <- a X + (b A + c A^2) X;  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * (the coefficients that the Muon optimiser published; from the other side where rows > cols), out = X: singular values of
+ * a thousandth of the norm and more come to lie between 0.7 and 1.2 in five steps.  x: dev float or bfloat16 (dtype); out: dev
+ * bfloat16, may be x.  The products take fp16 operands with fp32 sums, X itself is kept in 22 bits: results are within 0.4 % of
+ * the iteration in exact arithmetic (2-norm, five steps), rounding to bfloat16 included.  1 <= ns_steps <= 16; the shorter side at
+ * most 32,768, the longer at most 1,048,576. */
+int rlhf_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, size_t *out);
+int rlhf_orthogonalize(const void *x, int32_t dtype, int32_t batch, int32_t rows, int32_t cols, int32_t ns_steps, double eps,
+                       uint16_t *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One Muon step of weight matrices: rlhf_adamw_step's place for the matrices of the layers (vectors, embeddings and heads
+ * stay with AdamW).  For every tensor, g = grad * grad_scale:
+ *   m = momentum * m + (1 - momentum) g;   u = nesterov ? (1 - momentum) g + momentum * m : m
+ *   O = the orthogonalisation above of u;   p = (1 - lr * weight_decay) p - lr * rms * sqrt(max(rows, cols)) * O
+ * (an orthogonal factor's entries have the root mean square 1 / sqrt(max(rows, cols)), so that the step's is lr * rms whatever
+ * the shape; 0.2 is about AdamW's, and its learning rates then serve).  param, grad, momentum: dev float [rows, cols],
+ * contiguous; param_bf16: dev or NULL, receives the updated parameters rounded to bfloat16 (rlhf_refresh_weights as after
+ * rlhf_adamw_step).  tensors: HOST array of `count`, no two with the same arrays; ones without elements are skipped.  Matrices
+ * share launches; the workspace holds as many at a time as 2^28 elements are. */
+typedef struct {
+  float *param;
+  const float *grad;
+  float *momentum;
+  uint16_t *param_bf16;
+  int32_t rows, cols;
+} rlhf_muon_tensor;
+int rlhf_muon_workspace_bytes(const rlhf_muon_tensor *tensors, int32_t count, size_t *out);
+int rlhf_muon_step(const rlhf_muon_tensor *tensors, int32_t count, double lr, double momentum, int32_t nesterov,
+                   double weight_decay, double rms, int32_t ns_steps, double eps, double grad_scale, void *workspace,
+                   size_t workspace_bytes, void *stream);
 
 /* Backward pass through the output heads: from the gradients the loss head returns to the residual
  * stream after the last decoder layer and to the head parameters (paper: the PPO update trains the

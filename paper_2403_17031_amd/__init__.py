@@ -16,5 +16,9 @@ from .binding import (  # noqa: F401
     PPO_LOSS_STATS,
     adamw_step,
     attention_backward,
+    token_stats,
+    token_stats_backward,
+    orthogonalize,
+    muon_step,
     linear_lr,
 )

@@ -19,6 +19,9 @@ EXPORTS = (
     "rlhf_attention_branch_backward", "rlhf_attention_branch_backward_workspace_bytes",
     "rlhf_attention_backward_noalloc", "rlhf_weight_image_bytes", "rlhf_refresh_weights",
     "rlhf_ppo_update", "rlhf_ppo_update_workspace_bytes", "score_responses", "rlhf_score_responses_workspace_bytes",
+    "rlhf_token_stats", "rlhf_token_stats_workspace_bytes", "rlhf_token_stats_backward",
+    "rlhf_token_stats_backward_workspace_bytes", "rlhf_orthogonalize", "rlhf_orthogonalize_workspace_bytes",
+    "rlhf_muon_step", "rlhf_muon_workspace_bytes",
 )
 
 _PER_LAYER = ("ln1_g", "ln1_b", "ln2_g", "ln2_b", "w_qkv", "b_qkv", "w_o", "b_o", "w_fc1", "b_fc1", "w_fc2", "b_fc2")
@@ -61,6 +64,11 @@ class _UpdateConfig(C.Structure):  # rlhf_ppo_update_config
 
 class _TrainState(C.Structure):  # rlhf_train_state
     _fields_ = [("grads", _Grads), ("master", _Grads), ("exp_avg", _Grads), ("exp_avg_sq", _Grads)]
+
+
+class _MuonTensor(C.Structure):  # rlhf_muon_tensor
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("momentum", C.c_void_p), ("param_bf16", C.c_void_p),
+                ("rows", C.c_int32), ("cols", C.c_int32)]
 
 
 _lib = None
@@ -113,6 +121,15 @@ def load_library():
                                     vp, vp, vp, vp, vp, C.POINTER(i32), i32, vp, vp, sz, vp]
     lib.rlhf_attention_backward_noalloc.argtypes = [vp] * 5 + [i32] * 6 + [vp] * 3 + [vp]
     lib.rlhf_adamw_step.argtypes = [vp, vp, vp, vp, vp, u64, i32] + [C.c_double] * 6 + [vp]
+    i64, dbl = C.c_int64, C.c_double
+    lib.rlhf_token_stats_workspace_bytes.argtypes = [i32, i32, i32, i64, i64, i32, i32, C.POINTER(sz)]
+    lib.rlhf_token_stats.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, i32, f32, i32] + [vp] * 5 + [vp, sz, vp]
+    lib.rlhf_token_stats_backward_workspace_bytes.argtypes = [i32, i32, i32, i64, i64, i32, i32, C.POINTER(sz)]
+    lib.rlhf_token_stats_backward.argtypes = [vp, i64, vp, i64] + [vp] * 5 + [i32, i32, i32, i32, f32, i32, vp, vp, vp, sz, vp]
+    lib.rlhf_orthogonalize_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(sz)]
+    lib.rlhf_orthogonalize.argtypes = [vp, i32, i32, i32, i32, i32, dbl, vp, vp, sz, vp]
+    lib.rlhf_muon_workspace_bytes.argtypes = [C.POINTER(_MuonTensor), i32, C.POINTER(sz)]
+    lib.rlhf_muon_step.argtypes = [C.POINTER(_MuonTensor), i32, dbl, dbl, i32, dbl, dbl, i32, dbl, dbl, vp, sz, vp]
     lib.rlhf_last_error.restype = C.c_char_p
     for n in EXPORTS:
         if n not in ("rlhf_destroy", "rlhf_last_error"):
@@ -729,3 +746,157 @@ def adamw_step(param, grad, exp_avg, exp_avg_sq, step, lr=3e-6, beta1=0.9, beta2
         _check(lib.rlhf_adamw_step(param.data_ptr(), grad.data_ptr(), exp_avg.data_ptr(), exp_avg_sq.data_ptr(),
                                    None if param_bf16 is None else param_bf16.data_ptr(), n, int(step), lr, beta1, beta2,
                                    eps, weight_decay, grad_scale, _cur_stream(torch, dev)))
+
+
+# ---------------------------------------------------------------------- both ends of a policy update (stateless)
+def _scratch(torch, nbytes, device):
+    """Workspace of one call, from torch's allocator on the current stream of `device`."""
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if POISON:
+        ws.fill_(255)
+    return ws
+
+
+def _new(torch, shape, dtype, device):
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if POISON:
+        t.view(torch.uint8).fill_(255)
+    return t
+
+
+def _token_rows(torch, what, hidden, weight, targets):
+    """Checks the operands of the token statistics: (hidden, weight, targets, dtype code), rows contiguous, 16-byte aligned."""
+    codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    ts = (hidden, weight)
+    if any((not isinstance(t, torch.Tensor)) or not t.is_cuda or t.dim() != 2 for t in ts):
+        raise RlhfError(f"{what}: hidden and weight must be 2-D CUDA tensors")
+    if hidden.dtype not in codes or weight.dtype != hidden.dtype or weight.device != hidden.device:
+        raise RlhfError(f"{what}: hidden and weight must share a device and a dtype (float32, bfloat16 or float16)")
+    if hidden.shape[1] != weight.shape[1] or hidden.shape[1] == 0 or weight.shape[0] == 0:
+        raise RlhfError(f"{what}: hidden must be [T, d] and weight [V, d]")
+    d = hidden.shape[1]
+
+    def rows(t):  # any row stride goes; a column stride, overlapping rows or an odd base make a copy
+        ok = (t.stride(1) == 1 or d == 1) and (t.shape[0] <= 1 or t.stride(0) >= d) and t.data_ptr() % 16 == 0
+        return t if ok else t.contiguous().clone() if t.is_contiguous() else t.contiguous()
+
+    y = _dev_i32(torch, targets, hidden.device)
+    if tuple(y.shape) != (hidden.shape[0],):
+        raise RlhfError(f"{what}: targets must be [T]")
+    return rows(hidden), rows(weight), y, codes[hidden.dtype]
+
+
+def _ld(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def token_stats(hidden, weight, targets, temperature=1.0, top_k=0):
+    """Log-probabilities, entropies and alternatives of rows of hidden states [T, d] under an output matrix [V, d] (CUDA
+    tensors of one dtype, float32, bfloat16 or float16; rows may be strided); targets int32 [T], -1 for rows without one.
+    Returns a dict of CUDA tensors: logprobs, entropy and lse float32 [T] and, with top_k > 0, top_ids int32 and
+    top_logprobs float32 [T, top_k], most likely first, equal logits by lower id."""
+    import torch
+    lib = load_library()
+    h, w, y, code = _token_rows(torch, "token_stats", hidden, weight, targets)
+    (T, d), V, k, dev = h.shape, w.shape[0], int(top_k), h.device
+    res = {n: _new(torch, (T,), torch.float32, dev) for n in ("logprobs", "entropy", "lse")}
+    if k > 0:
+        res["top_ids"] = _new(torch, (T, k), torch.int32, dev)
+        res["top_logprobs"] = _new(torch, (T, k), torch.float32, dev)
+    need = C.c_size_t()
+    _check(lib.rlhf_token_stats_workspace_bytes(max(T, 1), d, V, _ld(h), _ld(w), code, k, C.byref(need)))
+    if T == 0:
+        return res
+    ws = _scratch(torch, need.value, dev)
+    _on_device(torch, dev, lib.rlhf_token_stats, h.data_ptr(), _ld(h), w.data_ptr(), _ld(w), y.data_ptr(), T, d, V, code,
+               float(temperature), k, res["logprobs"].data_ptr(), res["entropy"].data_ptr(), res["lse"].data_ptr(),
+               res["top_ids"].data_ptr() if k > 0 else None, res["top_logprobs"].data_ptr() if k > 0 else None,
+               ws.data_ptr(), need.value)
+    return res
+
+
+def token_stats_backward(hidden, weight, targets, lse, entropy, d_logprobs, d_entropy=None, temperature=1.0,
+                         grad_dtype=None):
+    """Gradients of the operands of token_stats from those of its log-probabilities and entropies: hidden, weight, targets and
+    temperature as in that call, lse and entropy its results, d_logprobs float32 [T], d_entropy float32 [T] or None (entropy is
+    not read then).  Returns a dict of CUDA tensors d_hidden [T, d] and d_weight [V, d], of the inputs' dtype or (grad_dtype)
+    float32."""
+    import torch
+    lib = load_library()
+    h, w, y, code = _token_rows(torch, "token_stats_backward", hidden, weight, targets)
+    (T, d), V, dev = h.shape, w.shape[0], h.device
+    dtype = h.dtype if grad_dtype is None else grad_dtype
+    if dtype not in (h.dtype, torch.float32):
+        raise RlhfError("token_stats_backward: grad_dtype must be the inputs' dtype or float32")
+    rows = [lse, d_logprobs] + ([] if d_entropy is None else [entropy, d_entropy])
+    rows = [None if a is None else _dev_f32(torch, a, dev) for a in rows]
+    if any(a is None or tuple(a.shape) != (T,) for a in rows):
+        raise RlhfError("token_stats_backward: lse, d_logprobs and, with d_entropy, entropy and d_entropy must be [T]")
+    need = C.c_size_t()
+    _check(lib.rlhf_token_stats_backward_workspace_bytes(max(T, 1), d, V, _ld(h), _ld(w), code, 0 if dtype == torch.float32 else code,
+                                                         C.byref(need)))
+    if T == 0:
+        return dict(d_hidden=_new(torch, (0, d), dtype, dev), d_weight=torch.zeros((V, d), dtype=dtype, device=dev))
+    res = dict(d_hidden=_new(torch, (T, d), dtype, dev), d_weight=_new(torch, (V, d), dtype, dev))
+    ws = _scratch(torch, need.value, dev)
+    ent, d_ent = (rows[2].data_ptr(), rows[3].data_ptr()) if d_entropy is not None else (None, None)
+    _on_device(torch, dev, lib.rlhf_token_stats_backward, h.data_ptr(), _ld(h), w.data_ptr(), _ld(w), y.data_ptr(),
+               rows[0].data_ptr(), ent, rows[1].data_ptr(), d_ent, T, d, V, code, float(temperature),
+               0 if dtype == torch.float32 else code, res["d_hidden"].data_ptr(), res["d_weight"].data_ptr(), ws.data_ptr(),
+               need.value)
+    return res
+
+
+def orthogonalize(x, ns_steps=5, eps=1e-7, out=None):
+    """Newton-Schulz orthogonalisation of a matrix [rows, cols] or a batch [batch, rows, cols]: a contiguous CUDA tensor,
+    float32 or bfloat16.  Returns a bfloat16 tensor of the same shape (or `out`, which may be x)."""
+    import torch
+    lib = load_library()
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() not in (2, 3) or not x.is_contiguous() or \
+            x.dtype not in (torch.float32, torch.bfloat16):
+        raise RlhfError("orthogonalize: x must be a contiguous CUDA tensor of 2 or 3 dimensions, float32 or bfloat16")
+    dev = x.device
+    if out is None:
+        out = _new(torch, x.shape, torch.bfloat16, dev)
+    elif out.dtype != torch.bfloat16 or out.shape != x.shape or out.device != dev or not out.is_contiguous():
+        raise RlhfError("orthogonalize: out must be a contiguous bfloat16 tensor of x's shape and device")
+    batch, (rows, cols) = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2:]
+    need = C.c_size_t()
+    if x.numel():
+        _check(lib.rlhf_orthogonalize_workspace_bytes(batch, rows, cols, C.byref(need)))
+        ws = _scratch(torch, need.value, dev)
+        _on_device(torch, dev, lib.rlhf_orthogonalize, x.data_ptr(), 0 if x.dtype == torch.float32 else 1, batch, rows, cols,
+                   int(ns_steps), float(eps), out.data_ptr(), ws.data_ptr(), need.value)
+    return out
+
+
+def muon_step(params, grads, momenta, lr=3e-6, momentum=0.95, nesterov=True, weight_decay=0.01, rms=0.2, ns_steps=5, eps=1e-7,
+              grad_scale=1.0, params_bf16=None):
+    """In-place Muon update of weight matrices: params, grads and momenta are lists of contiguous 2-D CUDA float32 tensors on
+    one device, matched by index; params_bf16: optional list of CUDA bfloat16 tensors that receive the rounded parameters.
+    The matrices of a call share its launches."""
+    import torch
+    lib = load_library()
+    lists = [list(params), list(grads), list(momenta)]
+    n = len(lists[0])
+    if any(len(v) != n for v in lists) or (params_bf16 is not None and len(params_bf16) != n):
+        raise RlhfError("muon_step: params, grads, momenta and params_bf16 must have the same length")
+    if n == 0:
+        return
+    bf = list(params_bf16) if params_bf16 is not None else [None] * n
+    dev = lists[0][0].device if isinstance(lists[0][0], torch.Tensor) else None
+    ts = (_MuonTensor * n)()
+    for i, (p, g, m, b) in enumerate(zip(*lists, bf)):
+        for t in (p, g, m):
+            if type(t) not in (torch.Tensor, torch.nn.Parameter) or t.dtype is not torch.float32 or t.dim() != 2 or \
+                    not t.is_cuda or t.device != dev or not t.is_contiguous() or t.shape != p.shape:
+                raise RlhfError("muon_step: params, grads and momenta must be contiguous 2-D CUDA float32 tensors of one shape "
+                                "each, all on one device")
+        if b is not None and (b.dtype is not torch.bfloat16 or b.shape != p.shape or b.device != dev or not b.is_contiguous()):
+            raise RlhfError("muon_step: params_bf16 must be contiguous CUDA bfloat16 tensors of the parameters' shapes")
+        ts[i] = _MuonTensor(p.data_ptr(), g.data_ptr(), m.data_ptr(), None if b is None else b.data_ptr(), p.shape[0], p.shape[1])
+    need = C.c_size_t()
+    _check(lib.rlhf_muon_workspace_bytes(ts, n, C.byref(need)))
+    ws = _scratch(torch, need.value, dev)
+    _on_device(torch, dev, lib.rlhf_muon_step, ts, n, float(lr), float(momentum), 1 if nesterov else 0, float(weight_decay),
+               float(rms), int(ns_steps), float(eps), float(grad_scale), ws.data_ptr(), need.value)

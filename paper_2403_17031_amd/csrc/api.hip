@@ -10,6 +10,8 @@
 
 #include "../../include/rlhf_rollout.h"
 #include "common.h"
+#include "muon.h"
+#include "token_stats.h"
 
 using namespace rlhf;
 
@@ -916,6 +918,245 @@ int rlhf_adamw_step(float* param, const float* grad, float* exp_avg, float* exp_
                     double grad_scale, void* stream) {
   const AdamwTensor t = {param, grad, exp_avg, exp_avg_sq, param_bf16, (size_t)n};
   return adamw_tensors(&t, 1, step, lr, beta1, beta2, eps, weight_decay, grad_scale, stream);
+}
+
+// ---- token statistics and their gradient ----
+static int check_token_shapes(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight, int32_t dtype) {
+  if (T <= 0 || d <= 0 || V <= 0) return fail(RLHF_EINVAL, "rows, width and vocabulary must be positive");
+  if (dtype != RLHF_DTYPE_FP32 && dtype != RLHF_DTYPE_BF16 && dtype != RLHF_DTYPE_FP16) return fail(RLHF_EUNSUPPORTED, "unknown dtype");
+  if (ld_hidden < d || ld_weight < d) return fail(RLHF_EINVAL, "row strides must be at least the width");
+  if (V > kMaxTokenVocab || d > (1 << 20) || ld_hidden > (1 << 22) || ld_weight > (1 << 22) || T > (1 << 26))
+    return fail(RLHF_EUNSUPPORTED, "vocabulary beyond 262,144, width beyond 2^20, row stride beyond 2^22 or rows beyond 2^26");
+  return RLHF_OK;
+}
+static TokenStatsArgs token_stats_args(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight, int32_t dtype, int32_t top_k) {
+  TokenStatsArgs a = {};
+  a.hidden = {nullptr, ld_hidden, token_rows_lie_well(ld_hidden, d, dtype, 0)};
+  a.weight = {nullptr, ld_weight, token_rows_lie_well(ld_weight, d, dtype, 0)};
+  a.T = T;
+  a.d = d;
+  a.V = V;
+  a.dtype = dtype;
+  a.top = top_k;
+  return a;
+}
+static int check_top(int32_t top_k, int32_t V) {
+  if (top_k < 0 || top_k > V) return fail(RLHF_EINVAL, "top_k must lie between 0 and the vocabulary");
+  if (top_k > kMaxTop) return fail(RLHF_EUNSUPPORTED, "top_k beyond 64");
+  return RLHF_OK;
+}
+
+int rlhf_token_stats_workspace_bytes(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight, int32_t dtype,
+                                     int32_t top_k, size_t* out) {
+  if (!out) return fail(RLHF_EINVAL, "null argument");
+  if (const int rc = check_token_shapes(T, d, V, ld_hidden, ld_weight, dtype)) return rc;
+  if (const int rc = check_top(top_k, V)) return rc;
+  *out = token_stats_plan(token_stats_args(T, d, V, ld_hidden, ld_weight, dtype, top_k), nullptr, nullptr, nullptr);
+  return RLHF_OK;
+}
+
+int rlhf_token_stats(const void* hidden, int64_t ld_hidden, const void* weight, int64_t ld_weight, const int32_t* targets,
+                     int32_t T, int32_t d, int32_t V, int32_t dtype, float temperature, int32_t top_k, float* out_logprobs,
+                     float* out_entropy, float* out_lse, int32_t* out_top_ids, float* out_top_logprobs, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  if (const int rc = rlhf_token_stats_workspace_bytes(T, d, V, ld_hidden, ld_weight, dtype, top_k, &need)) return rc;
+  if (!hidden || !weight || !targets || !out_logprobs || !out_entropy || !out_lse || !workspace)
+    return fail(RLHF_EINVAL, "null pointer argument");
+  if (top_k > 0 && (!out_top_ids || !out_top_logprobs)) return fail(RLHF_EINVAL, "top_k > 0 needs both of its outputs");
+  if (!(temperature > 0.f) || !std::isfinite(temperature)) return fail(RLHF_EINVAL, "temperature must be finite and > 0");
+  if ((((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)workspace) & 15) != 0)
+    return fail(RLHF_EINVAL, "matrices and workspace must be 16-byte aligned");
+  if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_token_stats_workspace_bytes reports");
+  TokenStatsArgs a = token_stats_args(T, d, V, ld_hidden, ld_weight, dtype, top_k);
+  a.hidden.p = hidden;
+  a.weight.p = weight;
+  a.targets = targets;
+  a.inv_t = 1.0f / temperature;
+  a.logprob = out_logprobs;
+  a.entropy = out_entropy;
+  a.lse = out_lse;
+  a.top_ids = out_top_ids;
+  a.top_logprob = out_top_logprobs;
+  hipError_t e = hipSuccess;
+  (void)token_stats_plan(a, workspace, (hipStream_t)stream, &e);
+  HIP_OK(e);
+  return RLHF_OK;
+}
+
+static TokenGradArgs token_grad_args(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight, int32_t dtype,
+                                     int32_t grad_dtype) {
+  TokenGradArgs a = {};
+  a.hidden = {nullptr, ld_hidden, token_rows_lie_well(ld_hidden, d, dtype, T)};
+  a.weight = {nullptr, ld_weight, token_rows_lie_well(ld_weight, d, dtype, V)};
+  a.T = T;
+  a.d = d;
+  a.V = V;
+  a.dtype = dtype;
+  a.grad_f32 = grad_dtype == RLHF_DTYPE_FP32;
+  return a;
+}
+
+int rlhf_token_stats_backward_workspace_bytes(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight,
+                                              int32_t dtype, int32_t grad_dtype, size_t* out) {
+  if (!out) return fail(RLHF_EINVAL, "null argument");
+  if (const int rc = check_token_shapes(T, d, V, ld_hidden, ld_weight, dtype)) return rc;
+  if (grad_dtype != dtype && grad_dtype != RLHF_DTYPE_FP32)
+    return fail(RLHF_EUNSUPPORTED, "gradients are of the inputs' type or fp32");
+  *out = token_stats_backward_plan(token_grad_args(T, d, V, ld_hidden, ld_weight, dtype, grad_dtype), nullptr, nullptr, nullptr);
+  return RLHF_OK;
+}
+
+int rlhf_token_stats_backward(const void* hidden, int64_t ld_hidden, const void* weight, int64_t ld_weight,
+                              const int32_t* targets, const float* lse, const float* entropy, const float* d_logprobs,
+                              const float* d_entropy, int32_t T, int32_t d, int32_t V, int32_t dtype, float temperature,
+                              int32_t grad_dtype, void* d_hidden, void* d_weight, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  size_t need = 0;
+  if (const int rc = rlhf_token_stats_backward_workspace_bytes(T, d, V, ld_hidden, ld_weight, dtype, grad_dtype, &need)) return rc;
+  if (!hidden || !weight || !targets || !lse || !d_logprobs || !d_hidden || !d_weight || !workspace || (d_entropy && !entropy))
+    return fail(RLHF_EINVAL, "null pointer argument");
+  if (!(temperature > 0.f) || !std::isfinite(temperature)) return fail(RLHF_EINVAL, "temperature must be finite and > 0");
+  if ((((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)workspace) & 15) != 0)
+    return fail(RLHF_EINVAL, "matrices and workspace must be 16-byte aligned");
+  if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_token_stats_backward_workspace_bytes reports");
+  TokenGradArgs a = token_grad_args(T, d, V, ld_hidden, ld_weight, dtype, grad_dtype);
+  a.hidden.p = hidden;
+  a.weight.p = weight;
+  a.targets = targets;
+  a.lse = lse;
+  a.entropy = entropy;
+  a.d_logprob = d_logprobs;
+  a.d_entropy = d_entropy;
+  a.inv_t = 1.0f / temperature;
+  a.d_hidden = d_hidden;
+  a.d_weight = d_weight;
+  hipError_t e = hipSuccess;
+  (void)token_stats_backward_plan(a, workspace, (hipStream_t)stream, &e);
+  HIP_OK(e);
+  return RLHF_OK;
+}
+
+// ---- orthogonalised updates ----
+static int check_muon_shape(int32_t rows, int32_t cols) {
+  if (std::min(rows, cols) > 32768 || std::max(rows, cols) > (1 << 20))
+    return fail(RLHF_EUNSUPPORTED, "a matrix's shorter side may have 32,768 entries, its longer 1,048,576");
+  return RLHF_OK;
+}
+static int check_ns(int32_t ns_steps, double eps) {
+  if (ns_steps < 1 || ns_steps > 16) return fail(RLHF_EINVAL, "ns_steps must lie between 1 and 16");
+  if (!(eps > 0.0) || !std::isfinite(eps)) return fail(RLHF_EINVAL, "eps must be finite and > 0");
+  return RLHF_OK;
+}
+
+int rlhf_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, size_t* out) {
+  if (!out) return fail(RLHF_EINVAL, "null argument");
+  if (batch <= 0 || rows <= 0 || cols <= 0) return fail(RLHF_EINVAL, "batch, rows and columns must be positive");
+  if (const int rc = check_muon_shape(rows, cols)) return rc;
+  MuonMatrix ms[kMuonGroup] = {};
+  const int n = std::min(batch, (int32_t)kMuonGroup);
+  for (int i = 0; i < n; ++i) ms[i].rows = rows, ms[i].cols = cols;
+  *out = muon_workspace_bytes(ms, n);
+  return RLHF_OK;
+}
+
+int rlhf_orthogonalize(const void* x, int32_t dtype, int32_t batch, int32_t rows, int32_t cols, int32_t ns_steps, double eps,
+                       uint16_t* out, void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  if (const int rc = rlhf_orthogonalize_workspace_bytes(batch, rows, cols, &need)) return rc;
+  if (!x || !out || !workspace) return fail(RLHF_EINVAL, "null pointer argument");
+  if (dtype != RLHF_DTYPE_FP32 && dtype != RLHF_DTYPE_BF16) return fail(RLHF_EUNSUPPORTED, "unknown dtype");
+  if (const int rc = check_ns(ns_steps, eps)) return rc;
+  if (((uintptr_t)x & (dtype == RLHF_DTYPE_FP32 ? 3 : 1)) != 0 || ((uintptr_t)out & 1) != 0 || ((uintptr_t)workspace & 15) != 0)
+    return fail(RLHF_EINVAL, "the workspace must be 16-byte aligned, the matrices as their elements");
+  if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_orthogonalize_workspace_bytes reports");
+  MuonScalars c = {};
+  c.src_bf16 = dtype == RLHF_DTYPE_BF16;
+  c.steps = ns_steps;
+  c.eps = (float)eps;
+  const size_t n = (size_t)rows * cols;
+  for (int32_t from = 0; from < batch; from += kMuonGroup) {
+    MuonMatrix ms[kMuonGroup] = {};
+    const int count = std::min(batch - from, (int32_t)kMuonGroup);
+    for (int i = 0; i < count; ++i) {
+      ms[i].src = (const char*)x + (size_t)(from + i) * n * (c.src_bf16 ? 2 : 4);
+      ms[i].out = out + (size_t)(from + i) * n;
+      ms[i].rows = rows;
+      ms[i].cols = cols;
+    }
+    HIP_OK(launch_muon(ms, count, c, workspace, (hipStream_t)stream));
+  }
+  return RLHF_OK;
+}
+
+// Up to kMuonGroup of the tensors from `from` on that have elements; `from` moves behind them.
+static int next_muon_tensors(const rlhf_muon_tensor* tensors, int32_t count, int32_t* from, MuonMatrix* ms) {
+  int n = 0;
+  for (; *from < count && n < kMuonGroup; ++*from) {
+    const rlhf_muon_tensor& t = tensors[*from];
+    if (t.rows == 0 || t.cols == 0) continue;
+    ms[n] = {};
+    ms[n].param = t.param;
+    ms[n].grad = t.grad;
+    ms[n].moment = t.momentum;
+    ms[n].param_bf16 = t.param_bf16;
+    ms[n].rows = t.rows;
+    ms[n++].cols = t.cols;
+  }
+  return n;
+}
+
+int rlhf_muon_workspace_bytes(const rlhf_muon_tensor* tensors, int32_t count, size_t* out) {
+  if (!out || (count > 0 && !tensors)) return fail(RLHF_EINVAL, "null argument");
+  if (count < 0) return fail(RLHF_EINVAL, "negative count");
+  for (int i = 0; i < count; ++i) {
+    if (tensors[i].rows < 0 || tensors[i].cols < 0) return fail(RLHF_EINVAL, "negative matrix dimension");
+    if (const int rc = check_muon_shape(tensors[i].rows, tensors[i].cols)) return rc;
+  }
+  *out = 0;
+  MuonMatrix ms[kMuonGroup];
+  for (int32_t from = 0; from < count;)
+    if (const int n = next_muon_tensors(tensors, count, &from, ms)) *out = std::max(*out, muon_workspace_bytes(ms, n));
+  return RLHF_OK;
+}
+
+int rlhf_muon_step(const rlhf_muon_tensor* tensors, int32_t count, double lr, double momentum, int32_t nesterov,
+                   double weight_decay, double rms, int32_t ns_steps, double eps, double grad_scale, void* workspace,
+                   size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  if (const int rc = rlhf_muon_workspace_bytes(tensors, count, &need)) return rc;
+  if (const int rc = check_ns(ns_steps, eps)) return rc;
+  if (!(momentum >= 0.0 && momentum < 1.0)) return fail(RLHF_EINVAL, "momentum must be in [0, 1)");
+  if (!(lr >= 0.0) || !(weight_decay >= 0.0) || !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(rms) ||
+      !std::isfinite(grad_scale))
+    return fail(RLHF_EINVAL, "lr and weight_decay must be finite and >= 0, rms and grad_scale finite");
+  for (int i = 0; i < count; ++i) {
+    const rlhf_muon_tensor& t = tensors[i];
+    if (t.rows == 0 || t.cols == 0) continue;
+    if (!t.param || !t.grad || !t.momentum) return fail(RLHF_EINVAL, "null pointer argument");
+    if ((((uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.momentum) & 3) != 0 || ((uintptr_t)t.param_bf16 & 1) != 0)
+      return fail(RLHF_EINVAL, "arrays must be aligned as their elements");
+    for (int k = 0; k < i; ++k)
+      if (tensors[k].rows > 0 && tensors[k].cols > 0 && (tensors[k].param == t.param || tensors[k].momentum == t.momentum))
+        return fail(RLHF_EINVAL, "two tensors share an array");
+  }
+  if (need == 0) return RLHF_OK;
+  if (!workspace) return fail(RLHF_EINVAL, "null pointer argument");
+  if (((uintptr_t)workspace & 15) != 0) return fail(RLHF_EINVAL, "the workspace must be 16-byte aligned");
+  if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_muon_workspace_bytes reports");
+  MuonScalars c = {};
+  c.nesterov = nesterov != 0;
+  c.steps = ns_steps;
+  c.beta = (float)momentum;
+  c.omb = (float)(1.0 - momentum);
+  c.grad_scale = (float)grad_scale;
+  c.eps = (float)eps;
+  c.decay = (float)(1.0 - lr * weight_decay);
+  c.lr_rms = lr * rms;
+  MuonMatrix ms[kMuonGroup];
+  for (int32_t from = 0; from < count;)
+    if (const int n = next_muon_tensors(tensors, count, &from, ms)) HIP_OK(launch_muon(ms, n, c, workspace, (hipStream_t)stream));
+  return RLHF_OK;
 }
 
 int rlhf_weight_image_bytes(const rlhf_model_config* cfg, size_t* out) {

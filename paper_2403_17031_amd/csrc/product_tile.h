@@ -1,0 +1,303 @@
+// Tiles of matrix products for the operators of an update (token_stats.hip, muon.hip): C[M,N] = sum_k A(m,k) W(n,k), in half,
+// bfloat16 or float, with an epilogue of the caller's, several products in one launch.
+//
+// Either operand is row-major (its rows hold k: a [M, K] or [N, K] matrix) or K-major ([K, M] or [K, N], so that a product
+// with a transposed matrix reads the matrix as it lies).  A stage is 128 bytes of k per row (64 k of 16-bit types, 32 of float),
+// brought from global memory straight to LDS; two stages alternate.  Row-major stages hold rows of 128 bytes whose
+// eight 16-byte chunks are XORed with bits 1..3 of the row, so that the 32 rows of an operand slice are read without
+// bank conflicts; K-major stages hold k-rows, chunk c of k-row k at c ^ 2(k mod 4), and 16-bit slices come from the
+// transposing LDS read (two of four k each).
+//
+// The loads of a stage are issued while the last quarter of the stage before it is multiplied and have a whole stage to
+// land; fragments of a quarter stage are read while the quarter before is multiplied.
+//
+// Rows past M or N repeat the last one and are not stored.  K is whole stages: operands that are not lie in
+// the caller's workspace with zeros up to there.  Row strides and bases are whole 16-byte chunks.
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+
+namespace rlhf {
+
+typedef __attribute__((ext_vector_type(16))) float pt_f32x16;
+typedef __attribute__((ext_vector_type(4))) float pt_f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t pt_u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t pt_u32x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 pt_f16x8;
+typedef __attribute__((ext_vector_type(8))) __bf16 pt_bf16x8;
+typedef __bf16 bfloat;
+
+// c += the outer products of two operand slices (16 bytes a lane: k = 16-byte chunk `lane / 32` of a pair of chunks)
+__device__ __forceinline__ pt_f32x16 pt_mma(half_t, pt_u32x4 w, pt_u32x4 a, pt_f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(pt_f16x8, w), __builtin_bit_cast(pt_f16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ pt_f32x16 pt_mma(bfloat, pt_u32x4 w, pt_u32x4 a, pt_f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pt_bf16x8, w), __builtin_bit_cast(pt_bf16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ pt_f32x16 pt_mma(float, pt_u32x4 w, pt_u32x4 a, pt_f32x16 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[e]), __uint_as_float(a[e]), c, 0, 0, 0);
+  return c;
+}
+
+#define PT_GLOBAL(p) ((const __attribute__((address_space(1))) void*)(p))
+#define PT_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+
+// WM x WN waves of MT x NT accumulators of 32 x 32
+template <int WM_, int WN_, int MT_, int NT_>
+struct PtShape {
+  static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_;
+  static constexpr int waves = WM * WN, rows = 32 * MT * WM, cols = 32 * NT * WN;
+};
+
+// One operand's tile loads: this lane's 16-byte chunks of a stage, as byte offsets from a uniform base.
+template <typename T, bool KM, int ROWS, int NW>
+struct PtLoads {
+  static constexpr int E = 16 / (int)sizeof(T), KD = 128 / (int)sizeof(T), L = ROWS / (8 * NW);
+  static constexpr int RB = KM ? ROWS * (int)sizeof(T) : 128;  // bytes of a stage's LDS row
+  const char* base;
+  uint32_t off[L];
+  size_t step;
+
+  __device__ static int lds_row(int i, int wave, int lane) { return (1024 * (L * wave + i) + 16 * lane) / RB; }
+  __device__ static int chunk(int i, int wave, int lane) {
+    const int r = lds_row(i, wave, lane), pos = ((1024 * (L * wave + i) + 16 * lane) % RB) / 16;
+    return KM ? pos ^ (2 * (r & 3)) : pos ^ ((r >> 1) & 7);
+  }
+  // the operand from its row r0 (of `extent`) on, from k0 on
+  __device__ void init(const void* p, uint32_t ld, int r0, int extent, int k0, int wave, int lane) {
+    const size_t stride = (size_t)ld * sizeof(T);
+    base = (const char*)p + (KM ? (size_t)k0 * stride + (size_t)r0 * sizeof(T) : (size_t)r0 * stride + (size_t)k0 * sizeof(T));
+    step = KM ? KD * stride : 128;
+    const int left = extent - r0;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const int r = lds_row(i, wave, lane), c = chunk(i, wave, lane);
+      off[i] = KM ? (uint32_t)(r * stride) + 16u * (uint32_t)min(c, (left - 1) / E)
+                  : (uint32_t)(min(r, left - 1) * stride) + 16u * (uint32_t)c;
+    }
+  }
+  __device__ __forceinline__ void load(char* lds, int stage, int i, int wave) const {
+    const char* p = base + stage * step;
+    asm volatile("" : "+s"(p));  // (uniform: a scalar base and the lane's 32-bit offset)
+    uint32_t o = off[i];
+    asm volatile("" : "+v"(o));
+    __builtin_amdgcn_global_load_lds(PT_GLOBAL(p + o), PT_LDS(lds + 1024 * (L * wave + i)), 16, 0, 0);
+  }
+};
+
+// Reads of an operand slice: 32 rows from row0 on, quarter stage s.
+template <typename T, bool KM, int ROWS>
+struct PtFrags {
+  static constexpr int RB = KM ? ROWS * (int)sizeof(T) : 128;
+  int at;
+  __device__ void init(int row0, int lane) {
+    const int l32 = lane & 31, hf = lane >> 5;
+    if constexpr (!KM) {
+      at = (row0 + l32) * 128;
+    } else if constexpr (sizeof(T) == 2) {
+      const int r = lane & 15, colb = row0 + 16 * ((lane >> 4) & 1);
+      const int c = ((colb >> 3) + ((r & 3) >> 1)) ^ (2 * ((r >> 2) & 3));
+      at = (8 * hf + (r >> 2)) * RB + c * 16 + (r & 1) * 8;
+    } else {
+      at = row0 + l32;  // column
+    }
+  }
+  __device__ __forceinline__ pt_u32x4 read(const char* lds, int s, int lane) const {
+    const int hf = lane >> 5;
+    if constexpr (!KM) {
+      const int key = ((lane & 31) >> 1) & 7;
+      return *(const pt_u32x4*)(lds + at + (((2 * s + hf) ^ key) << 4));
+    } else if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((ext_vector_type(4))) short s16x4;
+      typedef __attribute__((address_space(3))) s16x4* lds4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + at + 16 * s * RB));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + at + (16 * s + 4) * RB));
+      const pt_u32x2 l = __builtin_bit_cast(pt_u32x2, lo), h = __builtin_bit_cast(pt_u32x2, hi);
+      return pt_u32x4{l[0], l[1], h[0], h[1]};
+    } else {
+      pt_u32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int k = 8 * s + 4 * hf + e;
+        v[e] = *(const uint32_t*)(lds + k * RB + (((at >> 2) ^ (2 * (k & 3))) << 4) + (at & 3) * 4);
+      }
+      return v;
+    }
+  }
+};
+
+// acc = the product over k0 <= k < k1 of one tile; la*, lw*: the stages' LDS (separate variables, so that a read of one stage does not
+// wait for the loads into the other).  k1 - k0 is a positive multiple of a stage's depth.
+template <typename T, bool AK, bool WK, typename S>
+__device__ __forceinline__ void pt_product(const void* A, uint32_t lda, int m0, int M, const void* W, uint32_t ldw, int n0, int N,
+                                           int k0, int k1, char* la0, char* lw0, char* la1, char* lw1,
+                                           pt_f32x16 (&acc)[S::NT][S::MT]) {
+  constexpr int MT = S::MT, NT = S::NT, F = MT + NT, NMF = MT * NT;
+  using LA = PtLoads<T, AK, S::rows, S::waves>;
+  using LW = PtLoads<T, WK, S::cols, S::waves>;
+  constexpr int NL = LA::L + LW::L;
+  constexpr int STEPS = NMF > F ? (NMF > NL ? NMF : NL) : (F > NL ? F : NL);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / S::WN) * 32 * MT, wn = (wave % S::WN) * 32 * NT;
+  LA ga;
+  LW gw;
+  ga.init(A, lda, m0, M, k0, wave, lane);
+  gw.init(W, ldw, n0, N, k0, wave, lane);
+  PtFrags<T, AK, S::rows> ra[MT];
+  PtFrags<T, WK, S::cols> rw[NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) ra[i].init(wm + 32 * i, lane);
+#pragma unroll
+  for (int j = 0; j < NT; ++j) rw[j].init(wn + 32 * j, lane);
+  const int nk = (k1 - k0) / LA::KD;
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.f;
+  auto load_one = [&](char* la, char* lw, int stage, int n) {
+    if (n < LA::L) ga.load(la, stage, n, wave);
+    else gw.load(lw, stage, n - LA::L, wave);
+  };
+  auto load_all = [&](char* la, char* lw, int stage) {
+#pragma unroll
+    for (int n = 0; n < NL; ++n) load_one(la, lw, stage, n);
+  };
+  pt_u32x4 fa[2][MT], fw[2][NT];
+  auto frag = [&](const char* la, const char* lw, int s, int n, int buf) {
+    if (n < MT) fa[buf][n] = ra[n].read(la, s, lane);
+    else fw[buf][n - MT] = rw[n - MT].read(lw, s, lane);
+  };
+  // a quarter stage: the matrix instructions on fragments `buf`; between them the next quarter's fragment reads and, if LOAD,
+  // the tile loads of a later stage
+  auto sub = [&](int buf, const char* la, const char* lw, int s, auto load, char* da, char* dw, int stage) {
+    constexpr bool LOAD = decltype(load)::value;
+#pragma unroll
+    for (int n = 0; n < STEPS; ++n) {
+      if (n < NMF) {
+        const int j = n / MT, i = (j & 1) ? MT - 1 - n % MT : n % MT;  // serpentine: one operand changes at a time
+        acc[j][i] = pt_mma(T(), fw[buf][j], fa[buf][i], acc[j][i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (n < F) frag(la, lw, s, n, buf ^ 1);
+      if (LOAD && n < NL && stage < nk) load_one(da, dw, stage, n);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  using No = std::false_type;
+  using Yes = std::true_type;
+  // every wave's tile loads have landed and every wave has finished reading the current stage
+  auto wait = [&] {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // stage kt in (ca, cw); the next one is landing in (oa, ow)
+  auto stage = [&](int kt, char* ca, char* cw, char* oa, char* ow) {
+    sub(0, ca, cw, 1, No(), nullptr, nullptr, 0);
+    sub(1, ca, cw, 2, No(), nullptr, nullptr, 0);
+    sub(0, ca, cw, 3, No(), nullptr, nullptr, 0);
+    wait();
+    sub(1, oa, ow, 0, Yes(), ca, cw, kt + 2);  // (the last stage's fragments are of nothing, and not used)
+  };
+  load_all(la0, lw0, 0);
+  if (nk > 1) load_all(la1, lw1, 1);
+  wait();
+#pragma unroll
+  for (int n = 0; n < F; ++n) frag(la0, lw0, 0, n, 0);
+  int kt = 0;
+  for (; kt + 1 < nk; kt += 2) {
+    stage(kt, la0, lw0, la1, lw1);
+    stage(kt + 1, la1, lw1, la0, lw0);
+  }
+  if (kt < nk) stage(kt, la0, lw0, la1, lw1);
+}
+
+// The accumulators of a wave: element e of acc[j][i] is row 32 i + lane % 32, column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.
+__device__ __forceinline__ int pt_col(int j, int e, int hf) { return 32 * j + 8 * (e >> 2) + 4 * hf + (e & 3); }
+
+#define PT_WAVE_LDS_FENCE()                          \
+  __builtin_amdgcn_sched_barrier(0);                 \
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); \
+  __builtin_amdgcn_wave_barrier();                   \
+  __builtin_amdgcn_sched_barrier(0);
+
+// Hands a wave's results out in memory order.  value(j, i, e) are the elements in the accumulators' layout; sink(row, col, v) gets
+// 16 bytes of consecutive columns of a row of the wave's tile (a line's worth of a row from eight lanes); 32 rows at a time pass
+// through the wave's 4 KB of LDS (XOR-swizzled by row).  A direct store from the accumulators would touch 32 rows with 8 or 16
+// bytes each.
+template <int MT, typename V, typename O>
+__device__ __forceinline__ void pt_hand_out_16(char* ep, int lane, V value, O sink) {  // value: float -> 16 bits as uint16_t
+  const int l32 = lane & 31, hf = lane >> 5, rd_row = lane >> 3, rd_c = lane & 7;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint16_t h[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) h[u] = value(j, i, 4 * q + u);
+        const pt_u32x2 v = {(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16};
+        *(pt_u32x2*)(ep + l32 * 128 + (((4 * j + q) ^ (l32 & 7)) << 4) + 8 * hf) = v;
+      }
+    PT_WAVE_LDS_FENCE();
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const int row = 8 * it + rd_row;
+      sink(32 * i + row, rd_c * 8, *(const pt_u32x4*)(ep + row * 128 + ((rd_c ^ (row & 7)) << 4)));
+    }
+    PT_WAVE_LDS_FENCE();
+  }
+}
+template <int MT, int NT, typename V, typename O>
+__device__ __forceinline__ void pt_hand_out_32(char* ep, int lane, V value, O sink) {
+  const int l32 = lane & 31, hf = lane >> 5, rd_row = lane >> 3, rd_c = lane & 7;
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const pt_f32x4 v = {value(j, i, 4 * q), value(j, i, 4 * q + 1), value(j, i, 4 * q + 2), value(j, i, 4 * q + 3)};
+        *(pt_f32x4*)(ep + l32 * 128 + (((2 * q + hf) ^ (l32 & 7)) << 4)) = v;
+      }
+      PT_WAVE_LDS_FENCE();
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int row = 8 * it + rd_row;
+        sink(32 * i + row, 32 * j + rd_c * 4, *(const pt_f32x4*)(ep + row * 128 + ((rd_c ^ (row & 7)) << 4)));
+      }
+      PT_WAVE_LDS_FENCE();
+    }
+}
+
+// Tile t of nb_m x nb_n: consecutive tiles walk four row tiles for each column tile.
+__device__ __forceinline__ void pt_tile_pos(int t, int nb_m, int nb_n, int& tm, int& tn) {
+  constexpr int G = 4;
+  const int grp = t / (G * nb_n), r = t - grp * G * nb_n, gm = min(G, nb_m - grp * G);
+  tm = grp * G + r % gm;
+  tn = r / gm;
+}
+// Tile t of the lower triangle (tm >= tn) of a square of tiles.
+__device__ __forceinline__ void pt_tile_triangle(int t, int& tm, int& tn) {
+  tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+  while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
+  while (tm * (tm + 1) / 2 > t) --tm;
+  tn = t - tm * (tm + 1) / 2;
+}
+// Work item of this block of a launch of `items` (grid: a multiple of 8 that covers them): block b runs on XCD b % 8, and an
+// XCD takes a contiguous run of items, whose operands its L2 then holds.  -1: none.
+__device__ __forceinline__ int pt_item(int items) {
+  const int per = (items + 7) >> 3, b = (int)blockIdx.x, it = (b & 7) * per + (b >> 3);
+  return (b >> 3) < per && it < items ? it : -1;
+}
+inline unsigned pt_grid(int items) { return 8u * (unsigned)((items + 7) / 8); }
+
+}  // namespace rlhf

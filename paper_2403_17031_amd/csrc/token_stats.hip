@@ -1,0 +1,682 @@
+// Log-probabilities of given tokens, entropies and most likely alternatives of rows of hidden states under an output matrix,
+// and the gradient of the first two: logits l = h W^T (fp32 sums), z = l / temperature,
+//   lse = log sum_v exp z_v,  logprob = z_y - lse,  entropy = log S0 - S1 / S0
+//   with S0 = sum exp(z - max), S1 = sum exp(z - max) (z - max),
+//   dz_v = (g ([v = y] - p_v) - e p_v (log p_v + entropy)) / temperature,  dh = dz W,  dW = dz^T h.
+//
+// Forward: the product's epilogue leaves (max, S0, S1) of every part (the 64 columns of a wave) of a row, so without alternatives
+// no logit is stored.  With them the logits are stored, 4096 rows at a time, and read again at few places: an entry
+// among a row's k largest lies in one of the k parts whose maxima are largest (ties: the lower part, as the lower id among
+// equals), since each part before its own in that order holds an entry before it.  The second kernel picks those parts, then the
+// k entries among their 64 k logits.
+//
+// Backward: the first product's epilogue forms dz (rounded to the operands' type: products of 16-bit operands are what the
+// matrix cores run at full rate, and the rounding, half a step of 2^-8 or 2^-11 relative, is that of the results in the same
+// type); dh and dW read it row-major and K-major, W and h as they lie.
+#include <algorithm>
+
+#include "common.h"
+#include "product_tile.h"
+#include "token_stats.h"
+
+namespace rlhf {
+
+namespace {
+
+using PtBig = PtShape<2, 4, 4, 2>;  // 256 x 256, 8 waves of 128 x 64, a CU to itself (160 KB of LDS)
+using PtMid = PtShape<2, 2, 2, 2>;  // 128 x 128, 4 waves of 64 x 64, two blocks on a CU
+
+#define PT_SHARED(S)                                                  \
+  __shared__ __attribute__((aligned(16))) char la0[S::rows * 128];    \
+  __shared__ __attribute__((aligned(16))) char lw0[S::cols * 128];    \
+  __shared__ __attribute__((aligned(16))) char la1[S::rows * 128];    \
+  __shared__ __attribute__((aligned(16))) char lw1[S::cols * 128];    \
+  __shared__ __attribute__((aligned(16))) char lep[S::waves * 4096];
+
+constexpr int kPart = 64;  // columns of a part
+
+__device__ __forceinline__ uint32_t order_key(float v) {  // larger for larger values, -0 as +0, NaN below all
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  return v != v ? 0u : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float order_value(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
+}
+
+struct StatsArgs {
+  const void *h, *w;
+  uint32_t ldh, ldw;
+  int T, V, d;
+  const int32_t* targets;
+  float inv_t;
+  float *pmax, *ps0, *ps1;  // [part][T]
+  float* ztgt;              // [T], the target's logit
+  float* logits;            // [T][ldl] or null
+  int ldl;
+};
+
+template <typename T, typename S>
+__global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
+  PT_SHARED(S)
+  constexpr int MT = S::MT;
+  const int nb_m = (a.T + S::rows - 1) / S::rows, nb_n = (a.V + S::cols - 1) / S::cols;
+  const int item = pt_item(nb_m * nb_n);
+  if (item < 0) return;
+  int tm, tn;
+  pt_tile_pos(item, nb_m, nb_n, tm, tn);
+  pt_f32x16 acc[2][MT];
+  pt_product<T, false, false, S>(a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, la0, lw0, la1, lw1, acc);
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
+  const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
+  if (col0 >= a.V) return;
+  const int part = col0 / kPart;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int row = row0 + 32 * i + l32;
+    const bool in = row < a.T;
+    const int tcol = in ? a.targets[row] - col0 : -1;  // (an absent target is negative)
+    int lim = a.V - col0;  // columns of this wave that exist (opaque: 32 masks would otherwise be held in registers)
+    asm volatile("" : "+s"(lim));
+    float m = -INFINITY, zt = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int col = pt_col(j, e, hf);
+        const float v = acc[j][i][e];
+        zt = col == tcol ? v : zt;
+        m = fmaxf(m, col < lim ? v : -INFINITY);
+      }
+    m = half_max(m);
+    float s0 = 0.f, s1 = 0.f;
+    if (m > -INFINITY) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float t = (acc[j][i][e] - m) * a.inv_t;
+          float x = __expf(t);
+          x = pt_col(j, e, hf) < lim ? x : 0.f;
+          s0 += x;
+          s1 += x != 0.f ? x * t : 0.f;  // (0 times -infinity)
+        }
+    } else {  // -infinity alone, or NaN (which the maximum passes over)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (pt_col(j, e, hf) < lim && acc[j][i][e] != acc[j][i][e]) s0 = acc[j][i][e];
+    }
+    s0 = half_sum(s0);
+    s1 = half_sum(s1);
+    if (in) {
+      if (hf == 0) {
+        const size_t at = (size_t)part * a.T + row;
+        a.pmax[at] = m;
+        a.ps0[at] = s0;
+        a.ps1[at] = s1;
+      }
+      if (tcol >= 0 && tcol < 64 && ((tcol >> 2) & 1) == hf) a.ztgt[row] = zt;
+    }
+  }
+  if (a.logits) {  // (columns up to the row stride, a multiple of 64, exist)
+    char* const ep = lep + wave * 4096;
+    pt_hand_out_32<MT, 2>(
+        ep, lane, [&](int j, int i, int e) { return acc[j][i][e]; },
+        [&](int r, int c, pt_f32x4 v) {
+          if (row0 + r < a.T) *(pt_f32x4*)(a.logits + (size_t)(row0 + r) * a.ldl + col0 + c) = v;
+        });
+  }
+}
+
+// (max, S0, S1) of two sets of entries
+struct Stat {
+  float m, s0, s1;
+};
+__device__ __forceinline__ Stat stat_merge(Stat a, Stat b, float inv_t) {
+  const float m = fmaxf(a.m, b.m);
+  Stat r = {m, 0.f, 0.f};
+  auto add = [&](Stat x) {
+    if (x.m == -INFINITY) {  // nothing, or NaN alone
+      r.s0 += x.s0;
+      return;
+    }
+    const float t = (x.m - m) * inv_t, f = __expf(t);
+    r.s0 += f * x.s0;
+    r.s1 += f != 0.f ? f * (x.s1 + x.s0 * t) : 0.f;
+  };
+  add(a);
+  add(b);
+  return r;
+}
+
+struct FinishArgs {
+  const float *pmax, *ps0, *ps1, *ztgt, *logits;
+  const int32_t* targets;
+  int T, V, parts, ldl, top, rows;  // rows per block: 1, 4 or 16
+  float inv_t;
+  float *logprob, *entropy, *lse;
+  int32_t* top_ids;
+  float* top_logprob;
+};
+
+__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
+  auto step = [&](auto o) {
+    constexpr int O = decltype(o)::value;
+    const uint32_t lo = (uint32_t)lane_xor<O>((int)(uint32_t)v), hi = (uint32_t)lane_xor<O>((int)(uint32_t)(v >> 32));
+    const uint64_t x = (uint64_t)hi << 32 | lo;
+    v = x > v ? x : v;
+  };
+  step(std::integral_constant<int, 32>{});
+  step(std::integral_constant<int, 16>{});
+  step(std::integral_constant<int, 8>{});
+  step(std::integral_constant<int, 4>{});
+  step(std::integral_constant<int, 2>{});
+  step(std::integral_constant<int, 1>{});
+  return v;
+}
+
+// Block: `rows` rows, 256 / rows threads to each for the sums; then a wave per row for the alternatives.
+// LDS: the rows' part maxima [parts][rows + 1] (with alternatives), each wave's candidates [top * 64] and parts [top].
+__global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char dyn[];
+  __shared__ float sh[3][256];
+  __shared__ float row_lse[16];
+  const int tid = threadIdx.x, R = a.rows, G = 256 / R, r = tid % R, g = tid / R;
+  const int row = blockIdx.x * R + r;
+  const bool in = row < a.T;
+  float* const pm = (float*)dyn;
+  Stat s = {-INFINITY, 0.f, 0.f};
+  if (in) {
+    for (int p = g; p < a.parts; p += G) {
+      const size_t at = (size_t)p * a.T + row;
+      const Stat x = {a.pmax[at], a.ps0[at], a.ps1[at]};
+      if (a.top) pm[p * (R + 1) + r] = x.m;
+      s = stat_merge(s, x, a.inv_t);
+    }
+  }
+  for (int half = G / 2; half; half /= 2) {  // a fixed tree over the row's threads
+    sh[0][tid] = s.m;
+    sh[1][tid] = s.s0;
+    sh[2][tid] = s.s1;
+    __syncthreads();
+    if (g < half) s = stat_merge(s, Stat{sh[0][tid + half * R], sh[1][tid + half * R], sh[2][tid + half * R]}, a.inv_t);
+    __syncthreads();
+  }
+  if (g == 0 && in) {
+    const float ls = logf(s.s0), l = s.m * a.inv_t + ls;
+    row_lse[r] = l;
+    a.lse[row] = l;
+    a.entropy[row] = ls - s.s1 / s.s0;
+    const int y = a.targets[row];
+    a.logprob[row] = y >= 0 && y < a.V ? (a.ztgt[row] - s.m) * a.inv_t - ls : 0.f;
+  }
+  if (!a.top) return;
+  __syncthreads();
+  const int lane = tid & 63, wave = tid >> 6, kp = min(a.top, a.parts);
+  float* const cand = pm + a.parts * (R + 1) + wave * (a.top * (kPart + 1));
+  int* const sel = (int*)(cand + a.top * kPart);
+  for (int q = wave; q < R; q += 4) {
+    const int t = blockIdx.x * R + q;
+    if (t >= a.T) break;
+    uint64_t last = ~0ull;
+    for (int k = 0; k < kp; ++k) {
+      uint64_t best = 0;
+      for (int p = lane; p < a.parts; p += 64) {
+        const uint64_t x = (uint64_t)order_key(pm[p * (R + 1) + q]) << 32 | (0xFFFFFFFFu - (uint32_t)p);
+        if (x < last && x > best) best = x;
+      }
+      last = wave_max_u64(best);
+      if (lane == 0) sel[k] = (int)(0xFFFFFFFFu - (uint32_t)last);
+    }
+    PT_WAVE_LDS_FENCE();
+    for (int k = 0; k < kp; ++k) {
+      const int col = sel[k] * kPart + lane;
+      cand[k * kPart + lane] = col < a.V ? a.logits[(size_t)t * a.ldl + col] : 0.f;
+    }
+    const float lse = row_lse[q];
+    last = ~0ull;
+    for (int k = 0; k < a.top; ++k) {
+      uint64_t best = 0;
+      for (int j = 0; j < kp; ++j) {
+        const int col = sel[j] * kPart + lane;
+        const uint64_t x = (uint64_t)order_key(cand[j * kPart + lane]) << 32 | (0xFFFFFFFFu - (uint32_t)col);
+        if (col < a.V && x < last && x > best) best = x;
+      }
+      last = wave_max_u64(best);
+      if (lane == 0) {
+        a.top_ids[(size_t)t * a.top + k] = (int)(0xFFFFFFFFu - (uint32_t)last);
+        a.top_logprob[(size_t)t * a.top + k] = order_value((uint32_t)(last >> 32)) * a.inv_t - lse;
+      }
+    }
+    PT_WAVE_LDS_FENCE();
+  }
+}
+
+// dst [grid][ldd] = src [rows][cols] (row stride lds), zero beyond either
+template <typename T>
+__global__ void __launch_bounds__(256)
+    pack_rows_kernel(const T* __restrict__ src, size_t lds, int rows, int cols, T* __restrict__ dst, int ldd) {
+  const T* const s = src + (size_t)blockIdx.x * lds;
+  T* const o = dst + (size_t)blockIdx.x * ldd;
+  const int n = (int)blockIdx.x < rows ? cols : 0;
+  for (int c = threadIdx.x; c < ldd; c += 256) o[c] = c < n ? s[c] : (T)0.f;
+}
+
+// scale[0] = the power of two that brings the largest |dz| a row could have (|g| + 14 |e|, |log p + H| p being less) to 2^11 .. 2^12, well
+// inside fp16's range at either end; scale[1] = its reciprocal.
+__global__ void __launch_bounds__(1024) grad_scale_kernel(const int32_t* __restrict__ targets, const float* __restrict__ g,
+                                                          const float* __restrict__ e, int T, int V, float inv_t, float* __restrict__ scale) {
+  __shared__ float sh[16];
+  float m = 0.f;
+  for (int t = threadIdx.x; t < T; t += 1024) {
+    const float x = (targets[t] >= 0 && targets[t] < V ? fabsf(g[t]) : 0.f) + (e ? 14.f * fabsf(e[t]) : 0.f);
+    if (x < INFINITY) m = fmaxf(m, x);
+  }
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, sh[i]);
+    m *= inv_t;
+    int x = 12;
+    if (m > 0.f && m < INFINITY) (void)frexpf(m, &x);  // m < 2^x
+    x = min(max(12 - x, -60), 60);
+    scale[0] = ldexpf(1.f, x);
+    scale[1] = ldexpf(1.f, -x);
+  }
+}
+
+struct DzArgs {
+  const void *h, *w;
+  uint32_t ldh, ldw;
+  int T, V, d;
+  const int32_t* targets;
+  const float *lse, *entropy, *g, *e;  // e may be null
+  const float* scale;                  // null: 1
+  float inv_t;
+  void* dz;  // [rows][ldz], zero from T and V on
+  int ldz, rows;
+};
+
+__device__ __forceinline__ uint16_t bits_of(half_t, float v) { return __builtin_bit_cast(uint16_t, (half_t)v); }
+__device__ __forceinline__ uint16_t bits_of(bfloat, float v) { return __builtin_bit_cast(uint16_t, (bfloat)v); }
+
+template <typename T, typename S>
+__global__ void __launch_bounds__(64 * S::waves, 2) dz_kernel(DzArgs a) {
+  PT_SHARED(S)
+  constexpr int MT = S::MT;
+  const int nb_m = (a.T + S::rows - 1) / S::rows, nb_n = (a.V + S::cols - 1) / S::cols;
+  const int item = pt_item(nb_m * nb_n);
+  if (item < 0) return;
+  int tm, tn;
+  pt_tile_pos(item, nb_m, nb_n, tm, tn);
+  pt_f32x16 acc[2][MT];
+  pt_product<T, false, false, S>(a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, la0, lw0, la1, lw1, acc);
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
+  const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
+  char* const ep = lep + wave * 4096;
+  const float s = (a.scale ? a.scale[0] : 1.f) * a.inv_t;
+  int lim = a.V - col0;
+  asm volatile("" : "+s"(lim));
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const bool in = row0 + 32 * i + l32 < a.T;
+    const int row = min(row0 + 32 * i + l32, a.T - 1);
+    const int t = a.targets[row], y = t < a.V ? t : -1;
+    const float g = y >= 0 ? a.g[row] * s : 0.f, e = a.e ? a.e[row] * s : 0.f;
+    const float lse = a.lse[row], H = a.entropy[row];  // (H: anything without e)
+    const int tcol = y - col0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int col = pt_col(j, x, hf);
+        const float logp = fmaf(acc[j][i][x], a.inv_t, -lse), p = __expf(logp);
+        float v = p != 0.f ? -p * (g + e * (logp + H)) : 0.f;  // (0 times infinity)
+        if (logp != logp) v = logp;
+        v += y >= 0 && col == tcol ? g : 0.f;
+        acc[j][i][x] = in && col < lim ? v : 0.f;
+      }
+  }
+  if constexpr (sizeof(T) == 2) {
+    pt_hand_out_16<MT>(
+        ep, lane, [&](int j, int i, int e) { return bits_of(T(), acc[j][i][e]); },
+        [&](int r, int c, pt_u32x4 v) {
+          if (row0 + r < a.rows && col0 + c < a.ldz) *(pt_u32x4*)((T*)a.dz + (size_t)(row0 + r) * a.ldz + col0 + c) = v;
+        });
+  } else {
+    pt_hand_out_32<MT, 2>(
+        ep, lane, [&](int j, int i, int e) { return acc[j][i][e]; },
+        [&](int r, int c, pt_f32x4 v) {
+          if (row0 + r < a.rows && col0 + c < a.ldz) *(pt_f32x4*)((float*)a.dz + (size_t)(row0 + r) * a.ldz + col0 + c) = v;
+        });
+  }
+}
+
+// out [M, N] (T or float) = scale * A W', or the fp32 slabs of a product cut along K
+struct OutArgs {
+  const void *A, *W;
+  uint32_t lda, ldw;
+  int M, N, K, slices, k_slice;
+  const float* scale;  // null: 1
+  void* out;
+  size_t ldo;
+  int f32, add;  // out is float; added to what is there (float only)
+  float* slab;   // slices > 1: [slice][M][lds]
+  int lds;
+};
+
+template <typename T>
+__device__ __forceinline__ void out_store(const OutArgs& a, int row, int col, pt_f32x4 v, bool vec) {
+  if (a.slices > 1) return;
+  if (a.f32) {
+    float* const o = (float*)a.out + (size_t)row * a.ldo + col;
+    if (vec && col + 4 <= a.N) {
+      if (a.add) v += *(const pt_f32x4*)o;
+      *(pt_f32x4*)o = v;
+    } else {
+      for (int u = 0; u < 4; ++u)
+        if (col + u < a.N) o[u] = a.add ? o[u] + v[u] : v[u];
+    }
+  } else {
+    T* const o = (T*)a.out + (size_t)row * a.ldo + col;
+    for (int u = 0; u < 4; ++u)
+      if (col + u < a.N) o[u] = (T)v[u];
+  }
+}
+
+template <typename T, bool AK, bool WK, typename S>
+__global__ void __launch_bounds__(64 * S::waves, 2) out_kernel(OutArgs a) {
+  PT_SHARED(S)
+  constexpr int MT = S::MT;
+  const int nb_m = (a.M + S::rows - 1) / S::rows, nb_n = (a.N + S::cols - 1) / S::cols;
+  const int item = pt_item(nb_m * nb_n * a.slices);
+  if (item < 0) return;
+  const int z = item / (nb_m * nb_n);
+  int tm, tn;
+  pt_tile_pos(item - z * nb_m * nb_n, nb_m, nb_n, tm, tn);
+  pt_f32x16 acc[2][MT];
+  pt_product<T, AK, WK, S>(a.A, a.lda, tm * S::rows, a.M, a.W, a.ldw, tn * S::cols, a.N, z * a.k_slice,
+                           min(a.K, (z + 1) * a.k_slice), la0, lw0, la1, lw1, acc);
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
+  char* const ep = lep + wave * 4096;
+  if (a.slices > 1) {
+    float* const o = a.slab + (size_t)z * a.M * a.lds;
+    pt_hand_out_32<MT, 2>(
+        ep, lane, [&](int j, int i, int e) { return acc[j][i][e]; },
+        [&](int r, int c, pt_f32x4 v) {
+          if (row0 + r < a.M && col0 + c < a.lds) *(pt_f32x4*)(o + (size_t)(row0 + r) * a.lds + col0 + c) = v;
+        });
+    return;
+  }
+  const float s = a.scale ? a.scale[1] : 1.f;
+  const bool vec = ((uintptr_t)a.out & 15) == 0 && a.ldo % (a.f32 ? 4 : 8) == 0;
+  if (sizeof(T) == 2 && !a.f32 && vec) {
+    if constexpr (sizeof(T) == 2) {
+      pt_hand_out_16<MT>(
+          ep, lane, [&](int j, int i, int e) { return bits_of(T(), acc[j][i][e] * s); },
+          [&](int r, int c, pt_u32x4 v) {
+            if (row0 + r >= a.M) return;
+            uint16_t* const o = (uint16_t*)a.out + (size_t)(row0 + r) * a.ldo + col0 + c;
+            if (col0 + c + 8 <= a.N) {
+              *(pt_u32x4*)o = v;
+            } else {
+#pragma unroll
+              for (int u = 0; u < 8; ++u)
+                if (col0 + c + u < a.N) o[u] = (uint16_t)(v[u >> 1] >> (16 * (u & 1)));
+            }
+          });
+    }
+  } else {
+    pt_hand_out_32<MT, 2>(
+        ep, lane, [&](int j, int i, int e) { return acc[j][i][e] * s; },
+        [&](int r, int c, pt_f32x4 v) {
+          if (row0 + r < a.M) out_store<T>(a, row0 + r, col0 + c, v, vec);
+        });
+  }
+}
+
+// out = scale * the sum of the slabs in their order
+template <typename T>
+__global__ void __launch_bounds__(256) out_sum_kernel(OutArgs a) {
+  const int quads = a.lds / 4;
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (size_t)a.M * quads) return;
+  const int row = (int)(i / quads), col = (int)(i - (size_t)row * quads) * 4;
+  const float* const p = a.slab + (size_t)row * a.lds + col;
+  pt_f32x4 v = *(const pt_f32x4*)p;
+  for (int z = 1; z < a.slices; ++z) v += *(const pt_f32x4*)(p + (size_t)z * a.M * a.lds);
+  const float s = a.scale ? a.scale[1] : 1.f;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) v[u] *= s;
+  a.slices = 1;
+  out_store<T>(a, row, col, v, ((uintptr_t)a.out & 15) == 0 && a.ldo % 4 == 0);
+}
+
+// out (T) = a (float), n elements
+template <typename T>
+__global__ void __launch_bounds__(256) narrow_rows_kernel(const float* __restrict__ a, int cols, T* __restrict__ out, size_t ldo) {
+  for (int c = threadIdx.x; c < cols; c += 256) out[(size_t)blockIdx.x * ldo + c] = (T)a[(size_t)blockIdx.x * cols + c];
+}
+
+int tiles(int m, int n, int tm, int tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); }
+
+// The larger tile, whose operands are used twice as often, where its tiles fill the chip.
+bool big_tiles(int M, int N) { return tiles(M, N, 256, 256) >= 256; }
+
+struct Bump {
+  char* base;
+  size_t off = 0;
+  template <typename T>
+  T* take(size_t n) {
+    off = (off + 255) & ~(size_t)255;
+    T* const p = base ? (T*)(base + off) : nullptr;
+    off += n * sizeof(T);
+    return p;
+  }
+};
+
+size_t elem_size(int dtype) { return dtype == kTokensF32 ? 4 : 2; }
+int stage_of(int dtype) { return 128 / (int)elem_size(dtype); }  // k of a stage of the products
+int whole(int n, int stage) { return (n + stage - 1) / stage * stage; }
+int padded(int n) { return whole(n, 64); }
+
+constexpr int kLogitRows = 4096;   // rows of stored logits at a time
+constexpr int kGradRows = 16384;   // rows of dz at a time
+
+int equal_chunk(int T, int most) {  // rows of a chunk: as few chunks as there must be, of about the same size
+  const int n = (T + most - 1) / most;
+  return std::min(T, ((T + n - 1) / n + 127) & ~127);
+}
+
+template <typename F>
+void by_type(int dtype, F f) {
+  if (dtype == kTokensF32) f(float());
+  else if (dtype == kTokensBF16) f(bfloat());
+  else f(half_t());
+}
+
+struct Operand {
+  const void* p;
+  uint32_t ld;
+};
+// The matrix as the products read it: as it lies, or a copy in the workspace with zeros up to whole stages (p null: measuring).
+Operand packed(Bump& ws, const TokenRows& m, int rows, int d, int dtype, hipStream_t s) {
+  if (m.lies_well) return {m.p, (uint32_t)m.ld};
+  const int ldd = padded(d), rows_to = padded(rows);
+  char* const to = ws.take<char>((size_t)rows_to * ldd * elem_size(dtype));
+  if (to)
+    by_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      hipLaunchKernelGGL(pack_rows_kernel<T>, dim3(rows_to), dim3(256), 0, s, (const T*)m.p, (size_t)m.ld, rows, d, (T*)to, ldd);
+    });
+  return {to, (uint32_t)ldd};
+}
+
+size_t finish_lds(int parts, int rows, int top) { return top ? ((size_t)parts * (rows + 1) + (size_t)std::min(rows, 4) * top * (kPart + 1)) * 4 : 0; }
+
+}  // namespace
+
+bool token_rows_lie_well(int64_t ld, int d, int dtype, int rows_as_k) {
+  return ld % (16 / (int)elem_size(dtype)) == 0 && d % stage_of(dtype) == 0 && rows_as_k % stage_of(dtype) == 0;
+}
+
+size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s, hipError_t* err) {
+  Bump ws{(char*)workspace};
+  const int parts = (a.V + kPart - 1) / kPart;
+  const Operand h = packed(ws, a.hidden, a.T, a.d, a.dtype, s), w = packed(ws, a.weight, a.V, a.d, a.dtype, s);
+  const int rows = a.top ? equal_chunk(a.T, kLogitRows) : a.T;
+  StatsArgs k;
+  float* const part = ws.take<float>((size_t)3 * parts * rows);
+  float* const ztgt = ws.take<float>(rows);
+  float* const logits = a.top ? ws.take<float>((size_t)rows * padded(a.V)) : nullptr;
+  if (!workspace) return ws.off;
+  int R = rows >= 4096 ? 16 : rows >= 1024 ? 4 : 1;  // rows of a finishing block: many share the lines of the parts' sums
+  while (R > 1 && finish_lds(parts, R, a.top) > 60 * 1024) R /= 4;
+  for (int t0 = 0; t0 < a.T; t0 += rows) {
+    const int n = std::min(rows, a.T - t0);
+    k.h = (const char*)h.p + (size_t)t0 * h.ld * elem_size(a.dtype);
+    k.w = w.p;
+    k.ldh = h.ld;
+    k.ldw = w.ld;
+    k.T = n;
+    k.V = a.V;
+    k.d = whole(a.d, stage_of(a.dtype));
+    k.targets = a.targets + t0;
+    k.inv_t = a.inv_t;
+    k.pmax = part;
+    k.ps0 = part + (size_t)parts * n;
+    k.ps1 = k.ps0 + (size_t)parts * n;
+    k.ztgt = ztgt;
+    k.logits = logits;
+    k.ldl = padded(a.V);
+    by_type(a.dtype, [&](auto t) {
+      using T = decltype(t);
+      if (big_tiles(n, a.V))
+        hipLaunchKernelGGL((stats_kernel<T, PtBig>), dim3(pt_grid(tiles(n, a.V, 256, 256))), dim3(512), 0, s, k);
+      else
+        hipLaunchKernelGGL((stats_kernel<T, PtMid>), dim3(pt_grid(tiles(n, a.V, 128, 128))), dim3(256), 0, s, k);
+    });
+    FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, R, a.inv_t,
+                    a.logprob + t0, a.entropy + t0, a.lse + t0, a.top ? a.top_ids + (size_t)t0 * a.top : nullptr,
+                    a.top ? a.top_logprob + (size_t)t0 * a.top : nullptr};
+    hipLaunchKernelGGL(stats_finish_kernel, dim3((n + R - 1) / R), dim3(256), finish_lds(parts, R, a.top), s, f);
+    if ((*err = hipGetLastError()) != hipSuccess) return ws.off;
+  }
+  return ws.off;
+}
+
+// The slices of K of a product with few tiles: as many as make the rounds of 256 whole tiles (512 of the smaller) times a slice's length
+// shortest, each at least 512 long, with what the fp32 slabs cost to write and read again (5 TB/s against 1 PFLOP/s).
+static int out_slices(int M, int N, int K, int esz, int* k_slice) {
+  const bool big = big_tiles(M, N);
+  const int n0 = big ? tiles(M, N, 256, 256) : tiles(M, N, 128, 128), per = big ? 256 : 512, stage = 128 / esz;
+  const double flops = (big ? 2.0 * 65536 : 2.0 * 16384) * (esz == 4 ? 16 : 1) / 4e12 * (big ? 1 : 0.5);
+  int best = 1;
+  double best_t = 1e30;
+  for (int z = 1; z <= 64; ++z) {
+    const int q = ((K + z - 1) / z + stage - 1) / stage * stage;
+    if (z > 1 && (q < 512 || (K + q - 1) / q != z)) continue;
+    const double t = (double)((n0 * z + per - 1) / per) * q * flops + (z > 1 ? (double)z * M * N * 8 / 5e12 + 4e-6 : 0);
+    if (t < best_t) best_t = t, best = z;
+  }
+  *k_slice = ((K + best - 1) / best + stage - 1) / stage * stage;
+  return best;
+}
+
+template <typename T, bool AK, bool WK>
+static void launch_out(OutArgs& o, hipStream_t s) {
+  if (big_tiles(o.M, o.N))
+    hipLaunchKernelGGL((out_kernel<T, AK, WK, PtBig>), dim3(pt_grid(tiles(o.M, o.N, 256, 256) * o.slices)), dim3(512), 0, s, o);
+  else
+    hipLaunchKernelGGL((out_kernel<T, AK, WK, PtMid>), dim3(pt_grid(tiles(o.M, o.N, 128, 128) * o.slices)), dim3(256), 0, s, o);
+  if (o.slices > 1) {
+    const size_t n = (size_t)o.M * (o.lds / 4);
+    hipLaunchKernelGGL(out_sum_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, o);
+  }
+}
+
+size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStream_t s, hipError_t* err) {
+  Bump ws{(char*)workspace};
+  const Operand h = packed(ws, a.hidden, a.T, a.d, a.dtype, s), w = packed(ws, a.weight, a.V, a.d, a.dtype, s);
+  const int esz = (int)elem_size(a.dtype), stage = stage_of(a.dtype), rows = equal_chunk(a.T, kGradRows);
+  const int ldz = padded(a.V), kv = whole(a.V, stage), lds = (a.d + 3) & ~3;
+  const bool chunks = rows < a.T;
+  float* const scale = ws.take<float>(2);
+  char* const dz = ws.take<char>((size_t)whole(rows, stage) * ldz * esz);
+  // sums over several chunks of rows are formed in fp32: in the output, or here
+  const bool grads_f32 = a.grad_f32 || a.dtype == kTokensF32;
+  float* const dw32 = chunks && !grads_f32 ? ws.take<float>((size_t)a.V * a.d) : nullptr;
+  int kh = 0, kw = 0;
+  size_t slab = 0;
+  for (int t0 = 0; t0 < a.T; t0 += rows) {
+    const int n = std::min(rows, a.T - t0);
+    const int zh = out_slices(n, a.d, kv, esz, &kh), zw = out_slices(a.V, a.d, whole(n, stage), esz, &kw);
+    slab = std::max(slab, std::max(zh > 1 ? (size_t)zh * n * lds : 0, zw > 1 ? (size_t)zw * a.V * lds : 0));
+  }
+  float* const slabs = ws.take<float>(slab);
+  if (!workspace) return ws.off;
+  const bool scaled = a.dtype == kTokensF16;
+  if (scaled)
+    hipLaunchKernelGGL(grad_scale_kernel, dim3(1), dim3(1024), 0, s, a.targets, a.d_logprob, a.d_entropy, a.T, a.V, a.inv_t, scale);
+  for (int t0 = 0; t0 < a.T; t0 += rows) {
+    const int n = std::min(rows, a.T - t0);
+    const void* const hp = (const char*)h.p + (size_t)t0 * h.ld * esz;
+    const DzArgs k = {hp, w.p, h.ld, w.ld, n, a.V, whole(a.d, stage), a.targets + t0, a.lse + t0, (a.d_entropy ? a.entropy : a.lse) + t0, a.d_logprob + t0,
+                      a.d_entropy ? a.d_entropy + t0 : nullptr, scaled ? scale : nullptr, a.inv_t, dz, ldz, whole(n, stage)};
+    OutArgs oh = {}, ow = {};
+    oh.A = dz;
+    oh.lda = ldz;
+    oh.W = w.p;
+    oh.ldw = w.ld;
+    oh.M = n;
+    oh.N = a.d;
+    oh.K = kv;
+    oh.slices = out_slices(n, a.d, kv, esz, &oh.k_slice);
+    oh.out = (char*)a.d_hidden + (size_t)t0 * a.d * (grads_f32 ? 4 : 2);
+    oh.ldo = a.d;
+    oh.f32 = grads_f32;
+    ow.A = dz;
+    ow.lda = ldz;
+    ow.W = hp;
+    ow.ldw = h.ld;
+    ow.M = a.V;
+    ow.N = a.d;
+    ow.K = whole(n, stage);
+    ow.slices = out_slices(a.V, a.d, ow.K, esz, &ow.k_slice);
+    ow.out = dw32 ? (void*)dw32 : a.d_weight;
+    ow.ldo = a.d;
+    ow.f32 = grads_f32 || dw32;
+    ow.add = t0 > 0;
+    oh.scale = ow.scale = scaled ? scale : nullptr;
+    oh.slab = ow.slab = slabs;
+    oh.lds = ow.lds = lds;
+    by_type(a.dtype, [&](auto t) {
+      using T = decltype(t);
+      if (big_tiles(n, a.V))
+        hipLaunchKernelGGL((dz_kernel<T, PtBig>), dim3(pt_grid(tiles(n, a.V, 256, 256))), dim3(512), 0, s, k);
+      else
+        hipLaunchKernelGGL((dz_kernel<T, PtMid>), dim3(pt_grid(tiles(n, a.V, 128, 128))), dim3(256), 0, s, k);
+      launch_out<T, false, true>(oh, s);
+      launch_out<T, true, true>(ow, s);
+    });
+    if ((*err = hipGetLastError()) != hipSuccess) return ws.off;
+  }
+  if (dw32)
+    by_type(a.dtype, [&](auto t) {
+      using T = decltype(t);
+      hipLaunchKernelGGL(narrow_rows_kernel<T>, dim3(a.V), dim3(256), 0, s, (const float*)dw32, a.d, (T*)a.d_weight, (size_t)a.d);
+    });
+  *err = hipGetLastError();
+  return ws.off;
+}
+
+}  // namespace rlhf
