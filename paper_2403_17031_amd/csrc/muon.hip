@@ -42,6 +42,7 @@ struct Prob {
   MuonMatrix m;
   int rp, ld, sp;         // rows, columns, and the shorter of them, padded
   float step;             // lr rms sqrt(max(rows, cols))
+  int vec;                // 16-byte accesses to the caller's arrays: eight elements of a row start where they may
 };
 struct Group {
   Prob p[kProbs];
@@ -51,20 +52,63 @@ struct Group {
   MuonScalars c;
 };
 
-__device__ __forceinline__ int find_prob(const Group& g, uint32_t item) {
+// The problem of a work item, and the item's index within it.
+__device__ __forceinline__ const Prob& find_prob(const Group& g, uint32_t item, int& index) {
   int at = 0;
   for (int i = 1; i < g.count; ++i)
     if (g.first[i] <= item) at = i;
-  return at;
+  index = (int)(item - g.first[at]);
+  return g.p[at];
+}
+// Tiles: block b runs on XCD b % 8 and every XCD takes an eighth of each problem's tiles, a contiguous run, so that the XCDs
+// have the same work whatever the problems' sizes (first[] then counts eighths).  -1: none.
+__device__ __forceinline__ int find_tile(const Group& g, const Prob*& p) {
+  int index;
+  p = &find_prob(g, blockIdx.x >> 3, index);
+  const int at = (int)(p - g.p), eighth = (int)((at + 1 < g.count ? g.first[at + 1] : g.items) - g.first[at]);
+  return (int)(blockIdx.x & 7) * eighth + index;
 }
 
 __device__ __forceinline__ float bf16_at(const void* p, size_t i) { return __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16); }
+
+// v as two halves.  The value and its high half are kept opaque: a multiplication before the first rounding would be fused into it
+// for one of its uses and not for the other, and where the two roundings part, h and l would belong to different numbers, a whole
+// unit of h apart.
+__device__ __forceinline__ void split_halves(float v, half_t& h, half_t& l) {
+  asm volatile("" : "+v"(v));
+  float back = (float)(half_t)v;
+  asm volatile("" : "+v"(back));
+  h = (half_t)back;
+  l = (half_t)(v - back);
+}
 
 // What is orthogonalised at element i, from the updated momentum.
 __device__ __forceinline__ float source_at(const Prob& p, const MuonScalars& c, size_t i) {
   if (p.m.src) return c.src_bf16 ? bf16_at(p.m.src, i) : ((const float*)p.m.src)[i];
   const float v = p.m.moment[i];
   return c.nesterov ? c.omb * (c.grad_scale * p.m.grad[i]) + c.beta * v : v;
+}
+
+// The same of eight neighbours, all arrays 16-byte aligned there.
+__device__ __forceinline__ void source8(const Prob& p, const MuonScalars& c, size_t i, float (&v)[8]) {
+  if (p.m.src && c.src_bf16) {
+    const pt_u32x4 r = *(const pt_u32x4*)((const uint16_t*)p.m.src + i);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      v[2 * u] = __uint_as_float(r[u] << 16);
+      v[2 * u + 1] = __uint_as_float(r[u] & 0xFFFF0000u);
+    }
+    return;
+  }
+  const float* const src = p.m.src ? (const float*)p.m.src : p.m.moment;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const pt_f32x4 m = *(const pt_f32x4*)(src + i + 4 * k);
+    pt_f32x4 gr = {0.f, 0.f, 0.f, 0.f};
+    if (!p.m.src && c.nesterov) gr = *(const pt_f32x4*)(p.m.grad + i + 4 * k);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[4 * k + u] = !p.m.src && c.nesterov ? c.omb * (c.grad_scale * gr[u]) + c.beta * m[u] : m[u];
+  }
 }
 
 __device__ __forceinline__ double wave_sum_f64(double v) {
@@ -84,11 +128,33 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 // The momentum's update, and the sum of squares of 16,384 elements.
 __global__ void __launch_bounds__(256) muon_norm_kernel(Group g) {
   __shared__ double sh[4];
-  const int at = find_prob(g, blockIdx.x), block = (int)(blockIdx.x - g.first[at]);
-  const Prob& p = g.p[at];
+  int block;
+  const Prob& p = find_prob(g, blockIdx.x, block);
   const size_t n = (size_t)p.m.rows * p.m.cols, i0 = (size_t)block * kNormElems, i1 = min(n, i0 + kNormElems);
   double sum = 0.0;
-  for (size_t i = i0 + threadIdx.x; i < i1; i += 256) {
+  if (p.vec) {  // (i1 - i0 is a multiple of eight)
+    for (size_t i = i0 + 8 * threadIdx.x; i < i1; i += 2048) {
+      float v[8];
+      if (!p.m.src) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          pt_f32x4 m = *(const pt_f32x4*)(p.m.moment + i + 4 * k);
+          const pt_f32x4 gr = *(const pt_f32x4*)(p.m.grad + i + 4 * k);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            m[u] = g.c.beta * m[u] + g.c.omb * (g.c.grad_scale * gr[u]);
+            v[4 * k + u] = g.c.nesterov ? g.c.omb * (g.c.grad_scale * gr[u]) + g.c.beta * m[u] : m[u];
+          }
+          *(pt_f32x4*)(p.m.moment + i + 4 * k) = m;
+        }
+      } else {
+        source8(p, g.c, i, v);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum += (double)v[u] * (double)v[u];
+    }
+  }
+  for (size_t i = p.vec ? i1 : i0 + threadIdx.x; i < i1; i += 256) {
     if (!p.m.src) p.m.moment[i] = g.c.beta * p.m.moment[i] + g.c.omb * (g.c.grad_scale * p.m.grad[i]);
     const double v = source_at(p, g.c, i);
     sum += v * v;
@@ -114,110 +180,122 @@ __global__ void __launch_bounds__(256) muon_scale_kernel(Group g) {
   if (threadIdx.x == 0) *p.scale = (float)((double)kXScale / (sqrt(sh[0]) + (double)g.c.eps));
 }
 
-// X = scale * source as two halves, zero in the padding.  A block takes a row's 2048 columns.
+// X = scale * source as two halves, zero in the padding; eight columns a thread.
 __global__ void __launch_bounds__(256) muon_split_kernel(Group g) {
-  const int at = find_prob(g, blockIdx.x), block = (int)(blockIdx.x - g.first[at]);
-  const Prob& p = g.p[at];
-  const int per_row = (p.ld + 2047) / 2048, row = block / per_row, col = (block % per_row) * 2048 + threadIdx.x * 8;
-  if (col >= p.ld) return;
+  int block;
+  const Prob& p = find_prob(g, blockIdx.x, block);
+  const uint32_t chunk = (uint32_t)block * 256 + threadIdx.x, per_row = (uint32_t)p.ld / 8;
+  const uint32_t row = chunk / per_row, col = (chunk - row * per_row) * 8;
+  if (row >= (uint32_t)p.rp) return;
   const float s = *p.scale;
   typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
   f16x8 h, l;
+  float v[8];
+  const size_t at = (size_t)row * p.m.cols + col;
+  if (p.vec && row < (uint32_t)p.m.rows && col + 8 <= (uint32_t)p.m.cols) {
+    source8(p, g.c, at, v);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = row < (uint32_t)p.m.rows && col + u < (uint32_t)p.m.cols ? source_at(p, g.c, at + u) : 0.f;
+  }
 #pragma unroll
   for (int u = 0; u < 8; ++u) {
-    const float v = row < p.m.rows && col + u < p.m.cols ? s * source_at(p, g.c, (size_t)row * p.m.cols + col + u) : 0.f;
-    h[u] = (half_t)v;
-    l[u] = (half_t)(v - (float)h[u]);
+    half_t hu, lu;
+    split_halves(s * v[u], hu, lu);
+    h[u] = hu;
+    l[u] = lu;
   }
   *(f16x8*)(p.xh[0] + (size_t)row * p.ld + col) = h;
   *(f16x8*)(p.xl[0] + (size_t)row * p.ld + col) = l;
 }
 
-#define MUON_SHARED(S)                                                \
-  __shared__ __attribute__((aligned(16))) char la0[S::rows * 128];    \
-  __shared__ __attribute__((aligned(16))) char lw0[S::cols * 128];    \
-  __shared__ __attribute__((aligned(16))) char la1[S::rows * 128];    \
-  __shared__ __attribute__((aligned(16))) char lw1[S::cols * 128];    \
-  __shared__ __attribute__((aligned(16))) char lep[S::waves * 4096];
-
-__device__ __forceinline__ uint16_t f16_bits(float v) { return __builtin_bit_cast(uint16_t, (half_t)v); }
-
-// A symmetric tile: alpha * acc + beta * in (null: 0), stored at its place and, off the diagonal, mirrored.
-template <typename S>
+// A symmetric tile: alpha * acc + (IN) beta * in, stored at its place and, off the diagonal, mirrored.
+template <typename S, bool IN>
 __device__ __forceinline__ void store_symmetric(pt_f32x16 (&acc)[S::NT][S::MT], const half_t* in, half_t* out, int ld, int tm, int tn,
-                                                float alpha, float beta, char* lep) {
+                                                float alpha, float beta, char* ep) {
   constexpr int MT = S::MT;
+  typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
+  if (row0 >= ld || col0 >= ld) return;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int row = row0 + 32 * i + l32;
+    const int row = min(row0 + 32 * i + l32, ld - 1);
+    f16x4 x[2][4];
+    if (IN) {  // (a wave's 64 columns exist or do not as a whole)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[j][q] = *(const f16x4*)(in + (size_t)row * ld + col0 + pt_col(j, 4 * q, hf));
+    }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int col = col0 + pt_col(j, e, hf);
         float v = alpha * acc[j][i][e];
-        // (the input is symmetric too: read across, where neighbouring lanes' values are neighbours)
-        if (in && row < ld && col < ld) v += beta * (float)in[(size_t)col * ld + row];
+        if (IN) v += beta * (float)x[j][e >> 2][e & 3];
         acc[j][i][e] = v;
-        if (tm != tn && row < ld && col < ld) out[(size_t)col * ld + row] = (half_t)v;
       }
   }
-  pt_hand_out_16<MT>(
-      lep + wave * 4096, lane, [&](int j, int i, int e) { return f16_bits(acc[j][i][e]); },
-      [&](int r, int c, pt_u32x4 v) {
-        if (row0 + r < ld && col0 + c < ld) *(pt_u32x4*)(out + (size_t)(row0 + r) * ld + col0 + c) = v;
-      });
+  if (tm != tn)
+    pt_hand_out_transposed<MT>(ep, lane, acc, [&](int c, int r, pt_u32x4 v) {
+      if (row0 + r < ld) *(pt_u32x4*)(out + (size_t)(col0 + c) * ld + row0 + r) = v;
+    });
+  pt_hand_out<8, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, const float(&v)[8], int) {
+    if (row0 + r < ld) *(pt_u32x4*)(out + (size_t)(row0 + r) * ld + col0 + c) = pt_pack8<half_t>(v);
+  });
 }
 
 // A = X X^T (the shorter side's), scaled
 template <typename S>
 __global__ void __launch_bounds__(64 * S::waves, 2) muon_gram_kernel(Group g, int cur) {
-  MUON_SHARED(S)
-  const int item = pt_item(g.items);
-  if (item < 0) return;
-  const int at = find_prob(g, item);
-  const Prob& p = g.p[at];
+  PT_SHARED(S)
+  const Prob* pp;
+  const int tile = find_tile(g, pp);
+  const Prob& p = *pp;
   int tm, tn;
-  pt_tile_triangle(item - (int)g.first[at], tm, tn);
+  pt_tile_triangle(tile, tm, tn);
+  if (tm * S::rows >= p.sp) return;
   pt_f32x16 acc[S::NT][S::MT];
   const half_t* const x = p.xh[cur];
   if (p.m.rows > p.m.cols)
     pt_product<half_t, true, true, S>(x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp, la0, lw0, la1, lw1, acc);
   else
     pt_product<half_t, false, false, S>(x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld, la0, lw0, la1, lw1, acc);
-  store_symmetric<S>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f, lep);
+  store_symmetric<S, false>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f,
+                     pt_wave_lds<S>(la0, lw0, la1, lw1, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)));
 }
 
 // B = b A + c A^2
 template <typename S>
 __global__ void __launch_bounds__(64 * S::waves, 2) muon_poly_kernel(Group g) {
-  MUON_SHARED(S)
-  const int item = pt_item(g.items);
-  if (item < 0) return;
-  const int at = find_prob(g, item);
-  const Prob& p = g.p[at];
+  PT_SHARED(S)
+  const Prob* pp;
+  const int tile = find_tile(g, pp);
+  const Prob& p = *pp;
   int tm, tn;
-  pt_tile_triangle(item - (int)g.first[at], tm, tn);
+  pt_tile_triangle(tile, tm, tn);
+  if (tm * S::rows >= p.sp) return;
   pt_f32x16 acc[S::NT][S::MT];
   pt_product<half_t, false, false, S>(p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp, la0, lw0, la1, lw1, acc);
-  store_symmetric<S>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB, lep);
+  store_symmetric<S, true>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB,
+                     pt_wave_lds<S>(la0, lw0, la1, lw1, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)));
 }
 
 // X <- a X + B X, or after the last step what becomes of it
 template <typename S>
 __global__ void __launch_bounds__(64 * S::waves, 2) muon_update_kernel(Group g, int cur, int last) {
-  MUON_SHARED(S)
+  PT_SHARED(S)
   constexpr int MT = S::MT;
-  const int item = pt_item(g.items);
-  if (item < 0) return;
-  const int at = find_prob(g, item);
-  const Prob& p = g.p[at];
+  const Prob* pp;
+  const int tile = find_tile(g, pp);
+  const Prob& p = *pp;
+  const int nb_m = (p.rp + S::rows - 1) / S::rows, nb_n = (p.ld + S::cols - 1) / S::cols;
+  if (tile >= nb_m * nb_n) return;
   int tm, tn;
-  pt_tile_pos(item - (int)g.first[at], (p.rp + S::rows - 1) / S::rows, (p.ld + S::cols - 1) / S::cols, tm, tn);
+  pt_tile_pos(tile, nb_m, nb_n, tm, tn);
   pt_f32x16 acc[2][MT];
   if (p.m.rows > p.m.cols)
     pt_product<half_t, false, false, S>(p.xh[cur], p.ld, tm * S::rows, p.rp, p.b, p.sp, tn * S::cols, p.sp, 0, p.sp, la0, lw0, la1,
@@ -229,40 +307,70 @@ __global__ void __launch_bounds__(64 * S::waves, 2) muon_update_kernel(Group g, 
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
-  typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
-  const int rows = p.m.rows, cols = p.m.cols;
-  pt_hand_out_32<MT, 2>(
-      lep + wave * 4096, lane, [&](int j, int i, int e) { return acc[j][i][e]; },
-      [&](int r, int c, pt_f32x4 v) {
+  if (row0 >= p.rp || col0 >= p.ld) return;
+  typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+  const int rows = p.m.rows, cols = p.m.cols, rd_row = lane >> 3, rd_c = lane & 7;
+  const half_t* const xh = p.xh[cur] + (size_t)row0 * p.ld + col0;
+  const half_t* const xl = p.xl[cur] + (size_t)row0 * p.ld + col0;
+  half_t* const nh = p.xh[cur ^ 1] + (size_t)row0 * p.ld + col0;
+  half_t* const nl = p.xl[cur ^ 1] + (size_t)row0 * p.ld + col0;
+  f16x8 h[8], l[8];  // this pass's X, requested before the results go through LDS
+  pt_hand_out<8, MT>(
+      pt_wave_lds<S>(la0, lw0, la1, lw1, wave), lane, acc,
+      [&](int pass) {
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+          const size_t i = (size_t)min(64 * pass + 8 * it + rd_row, p.rp - 1 - row0) * p.ld + 8 * rd_c;
+          h[it] = *(const f16x8*)(xh + i);
+          l[it] = *(const f16x8*)(xl + i);
+        }
+      },
+      [&](int r, int c, float(&v)[8], int it) {
         const int row = row0 + r, col = col0 + c;
-        if (row >= p.rp || col >= p.ld) return;
-        const size_t i = (size_t)row * p.ld + col;
-        const f16x4 h = *(const f16x4*)(p.xh[cur] + i), l = *(const f16x4*)(p.xl[cur] + i);
+        if (row >= p.rp) return;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = fmaf(v[u], 1.f / kAScale, kA * ((float)h[u] + (float)l[u]));
+        for (int u = 0; u < 8; ++u) v[u] = fmaf(v[u], 1.f / kAScale, kA * ((float)h[it][u] + (float)l[it][u]));
         if (!last) {
-          f16x4 nh, nl;
+          f16x8 a, b;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            nh[u] = (half_t)v[u];
-            nl[u] = (half_t)(v[u] - (float)nh[u]);
+          for (int u = 0; u < 8; ++u) {
+            half_t hu, lu;
+            split_halves(v[u], hu, lu);
+            a[u] = hu;
+            b[u] = lu;
           }
-          *(f16x4*)(p.xh[cur ^ 1] + i) = nh;
-          *(f16x4*)(p.xl[cur ^ 1] + i) = nl;
+          const size_t i = (size_t)r * p.ld + c;
+          *(f16x8*)(nh + i) = a;
+          *(f16x8*)(nl + i) = b;
           return;
         }
         if (row >= rows) return;
         const size_t o = (size_t)row * cols + col;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 8; ++u) v[u] *= 1.f / kXScale;
+        if (p.vec && col + 8 <= cols) {
+          if (!p.m.src) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              pt_f32x4 w = *(const pt_f32x4*)(p.m.param + o + 4 * k);
+#pragma unroll
+              for (int u = 0; u < 4; ++u) v[4 * k + u] = w[u] = g.c.decay * w[u] - p.step * v[4 * k + u];
+              *(pt_f32x4*)(p.m.param + o + 4 * k) = w;
+            }
+          }
+          uint16_t* const to = p.m.src ? p.m.out : p.m.param_bf16;
+          if (to) *(pt_u32x4*)(to + o) = pt_pack8<bfloat>(v);
+          return;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
           if (col + u >= cols) break;
-          const float x = v[u] * (1.f / kXScale);
           if (p.m.src) {
-            p.m.out[o + u] = __builtin_bit_cast(uint16_t, (bfloat)x);
+            p.m.out[o + u] = pt_bits(bfloat(), v[u]);
           } else {
-            const float w = g.c.decay * p.m.param[o + u] - p.step * x;
+            const float w = g.c.decay * p.m.param[o + u] - p.step * v[u];
             p.m.param[o + u] = w;
-            if (p.m.param_bf16) p.m.param_bf16[o + u] = __builtin_bit_cast(uint16_t, (bfloat)w);
+            if (p.m.param_bf16) p.m.param_bf16[o + u] = pt_bits(bfloat(), w);
           }
         }
       });
@@ -321,6 +429,36 @@ void number(Group& g, F items) {
 int up(int n, int t) { return (n + t - 1) / t; }
 int triangle(int n) { return n * (n + 1) / 2; }
 
+// What runs on tiles: the number of them and the length of their sums.
+struct Tiles {
+  int (*count)(const Prob&, int tile);
+  int (*depth)(const Prob&);
+};
+const Tiles kGram = {[](const Prob& p, int t) { return triangle(up(p.sp, t)); }, [](const Prob& p) { return std::max(p.rp, p.ld); }};
+const Tiles kPoly = {[](const Prob& p, int t) { return triangle(up(p.sp, t)); }, [](const Prob& p) { return p.sp; }};
+const Tiles kUpdate = {[](const Prob& p, int t) { return up(p.rp, t) * up(p.ld, t); }, [](const Prob& p) { return p.sp; }};
+
+// Rounds that the tiles take on `slots` places, in units of the deepest tile's time.
+double rounds(const Group& g, const Tiles& t, int tile, int slots) {
+  double work = 0, most = 0;
+  for (int i = 0; i < g.count; ++i) {
+    work += (double)t.count(g.p[i], tile) * t.depth(g.p[i]);
+    most = std::max(most, (double)t.depth(g.p[i]));
+  }
+  return std::ceil(work / most / slots);
+}
+// The larger tile makes four times the smaller's products in 1.3 times what two smaller ones on a CU take (1.95 and 1.5 us a
+// stage).
+bool takes_big(const Group& g, const Tiles& t) { return 1.3 * rounds(g, t, 256, 256) <= rounds(g, t, 128, 512); }
+
+template <typename K, typename... A>
+void on_tiles(Group& g, const Tiles& t, hipStream_t s, K big, K mid, A... args) {
+  const bool b = takes_big(g, t);
+  number(g, [&](const Prob& p) { return up(t.count(p, b ? 256 : 128), 8); });
+  if (b) hipLaunchKernelGGL(big, dim3(8 * g.items), dim3(64 * PtBig::waves), 0, s, g, args...);
+  else hipLaunchKernelGGL(mid, dim3(8 * g.items), dim3(64 * PtMid::waves), 0, s, g, args...);
+}
+
 }  // namespace
 
 size_t muon_workspace_bytes(const MuonMatrix* ms, int count) {
@@ -343,19 +481,21 @@ hipError_t launch_muon(const MuonMatrix* ms, int count, const MuonScalars& c, vo
     for (int i = 0; i < g.count; ++i) {
       const MuonMatrix& m = g.p[i].m = ms[from + i];
       g.p[i].step = (float)(c.lr_rms * std::sqrt((double)std::max(m.rows, m.cols)));
+      const uintptr_t bases = (uintptr_t)m.src | (uintptr_t)m.out | (uintptr_t)m.param | (uintptr_t)m.grad | (uintptr_t)m.moment |
+                              (uintptr_t)m.param_bf16;
+      g.p[i].vec = m.cols % 8 == 0 && (bases & 15) == 0;
     }
+    std::sort(g.p, g.p + g.count, [](const Prob& a, const Prob& b) { return std::max(a.rp, a.ld) > std::max(b.rp, b.ld); });
     number(g, [](const Prob& p) { return norm_blocks(p.m.rows, p.m.cols); });
     hipLaunchKernelGGL(muon_norm_kernel, dim3(g.items), dim3(256), 0, s, g);
     hipLaunchKernelGGL(muon_scale_kernel, dim3(g.count), dim3(256), 0, s, g);
-    number(g, [](const Prob& p) { return p.rp * up(p.ld, 2048); });
+    number(g, [](const Prob& p) { return (int)(((size_t)p.rp * p.ld / 8 + 255) / 256); });
     hipLaunchKernelGGL(muon_split_kernel, dim3(g.items), dim3(256), 0, s, g);
     for (int k = 0; k < c.steps; ++k) {
       const int cur = k & 1;
-      number(g, [](const Prob& p) { return triangle(up(p.sp, PtMid::rows)); });
-      hipLaunchKernelGGL(muon_gram_kernel<PtMid>, dim3(pt_grid(g.items)), dim3(64 * PtMid::waves), 0, s, g, cur);
-      hipLaunchKernelGGL(muon_poly_kernel<PtMid>, dim3(pt_grid(g.items)), dim3(64 * PtMid::waves), 0, s, g);
-      number(g, [](const Prob& p) { return up(p.rp, PtMid::rows) * up(p.ld, PtMid::cols); });
-      hipLaunchKernelGGL(muon_update_kernel<PtMid>, dim3(pt_grid(g.items)), dim3(64 * PtMid::waves), 0, s, g, cur, k + 1 == c.steps);
+      on_tiles(g, kGram, s, muon_gram_kernel<PtBig>, muon_gram_kernel<PtMid>, cur);
+      on_tiles(g, kPoly, s, muon_poly_kernel<PtBig>, muon_poly_kernel<PtMid>);
+      on_tiles(g, kUpdate, s, muon_update_kernel<PtBig>, muon_update_kernel<PtMid>, cur, (int)(k + 1 == c.steps));
     }
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     from = to;

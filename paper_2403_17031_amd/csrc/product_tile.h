@@ -228,59 +228,123 @@ __device__ __forceinline__ int pt_col(int j, int e, int hf) { return 32 * j + 8 
   __builtin_amdgcn_wave_barrier();                   \
   __builtin_amdgcn_sched_barrier(0);
 
-// Hands a wave's results out in memory order.  value(j, i, e) are the elements in the accumulators' layout; sink(row, col, v) gets
-// 16 bytes of consecutive columns of a row of the wave's tile (a line's worth of a row from eight lanes); 32 rows at a time pass
-// through the wave's 4 KB of LDS (XOR-swizzled by row).  A direct store from the accumulators would touch 32 rows with 8 or 16
-// bytes each.
-template <int MT, typename V, typename O>
-__device__ __forceinline__ void pt_hand_out_16(char* ep, int lane, V value, O sink) {  // value: float -> 16 bits as uint16_t
-  const int l32 = lane & 31, hf = lane >> 5, rd_row = lane >> 3, rd_c = lane & 7;
+// The stages' LDS of a block: operands of stage 0 and of stage 1 (see pt_product).
+#define PT_SHARED(S)                                               \
+  __shared__ __attribute__((aligned(16))) char la0[S::rows * 128]; \
+  __shared__ __attribute__((aligned(16))) char lw0[S::cols * 128]; \
+  __shared__ __attribute__((aligned(16))) char la1[S::rows * 128]; \
+  __shared__ __attribute__((aligned(16))) char lw1[S::cols * 128];
+
+// After the product a wave has 16 KB of it to itself: every wave has passed the last barrier with all that it read of the stages.
+template <typename S>
+__device__ __forceinline__ char* pt_wave_lds(char* la0, char* lw0, char* la1, char* lw1, int wave) {
+  static_assert(S::rows == S::cols && S::rows * 512 == S::waves * 16384, "16 KB a wave");
+  constexpr int per = S::waves / 4;
+  char* const base = wave / per == 0 ? la0 : wave / per == 1 ? lw0 : wave / per == 2 ? la1 : lw1;
+  return base + wave % per * 16384;
+}
+
+// Hands a wave's results out in memory order: 64 rows of its 64 columns at a time pass through its LDS as float (16-byte chunks XORed with
+// the row), since a store from the accumulators would touch 32 rows with 16 bytes each.  sink(row, col, v, it): N (4 or 8)
+// consecutive columns of a row, sixteen or eight lanes a row, the pass's it-th call; before(pass): called before a pass's 64 rows.
+template <int N, int MT, typename B, typename O>
+__device__ __forceinline__ void pt_hand_out(char* ep, int lane, const pt_f32x16 (&acc)[2][MT], B before, O sink) {
+  static_assert(MT % 2 == 0 && (N == 4 || N == 8), "64 rows");
+  const int l32 = lane & 31, hf = lane >> 5;
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
+  for (int pass = 0; pass < MT / 2; ++pass) {
+    before(pass);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint16_t h[4];
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) h[u] = value(j, i, 4 * q + u);
-        const pt_u32x2 v = {(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16};
-        *(pt_u32x2*)(ep + l32 * 128 + (((4 * j + q) ^ (l32 & 7)) << 4) + 8 * hf) = v;
-      }
+        for (int q = 0; q < 4; ++q) {
+          const pt_f32x16& a = acc[j][2 * pass + i];
+          const pt_f32x4 v = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+          *(pt_f32x4*)(ep + (32 * i + l32) * 256 + (((8 * j + 2 * q + hf) ^ (l32 & 15)) << 4)) = v;
+        }
     PT_WAVE_LDS_FENCE();
+    constexpr int LR = 64 / N, RI = 64 / LR;  // lanes of a row, rows of an instruction
+    const int rd_row = lane / LR, rd_c = lane % LR;
 #pragma unroll
-    for (int it = 0; it < 4; ++it) {
-      const int row = 8 * it + rd_row;
-      sink(32 * i + row, rd_c * 8, *(const pt_u32x4*)(ep + row * 128 + ((rd_c ^ (row & 7)) << 4)));
+    for (int it = 0; it < 64 / RI; ++it) {
+      const int row = RI * it + rd_row;
+      if constexpr (N == 4) {
+        sink(64 * pass + row, rd_c * 4, *(const pt_f32x4*)(ep + row * 256 + ((rd_c ^ (row & 15)) << 4)), it);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const pt_f32x4 x = *(const pt_f32x4*)(ep + row * 256 + (((2 * rd_c + k) ^ (row & 15)) << 4));
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[4 * k + u] = x[u];
+        }
+        sink(64 * pass + row, rd_c * 8, v, it);
+      }
     }
     PT_WAVE_LDS_FENCE();
   }
 }
-template <int MT, int NT, typename V, typename O>
-__device__ __forceinline__ void pt_hand_out_32(char* ep, int lane, V value, O sink) {
-  const int l32 = lane & 31, hf = lane >> 5, rd_row = lane >> 3, rd_c = lane & 7;
+struct PtNothing {
+  __device__ void operator()(int) const {}
+};
+
+// The transpose of a wave's results as half: sink(col, row, v) gets eight consecutive rows of a column.  32 MT rows of 128 bytes in LDS,
+// read through the transposing LDS read (see PtFrags).
+template <int MT, typename O>
+__device__ __forceinline__ void pt_hand_out_transposed(char* ep, int lane, const pt_f32x16 (&acc)[2][MT], O sink) {
+  typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+  typedef __attribute__((ext_vector_type(4))) short s16x4;
+  typedef __attribute__((address_space(3))) s16x4* lds4;
+  const int l32 = lane & 31, hf = lane >> 5;
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const pt_f32x4 v = {value(j, i, 4 * q), value(j, i, 4 * q + 1), value(j, i, 4 * q + 2), value(j, i, 4 * q + 3)};
-        *(pt_f32x4*)(ep + l32 * 128 + (((2 * q + hf) ^ (l32 & 7)) << 4)) = v;
-      }
-      PT_WAVE_LDS_FENCE();
+        f16x4 h;
 #pragma unroll
-      for (int it = 0; it < 4; ++it) {
-        const int row = 8 * it + rd_row;
-        sink(32 * i + row, 32 * j + rd_c * 4, *(const pt_f32x4*)(ep + row * 128 + ((rd_c ^ (row & 7)) << 4)));
+        for (int u = 0; u < 4; ++u) h[u] = (half_t)acc[j][i][4 * q + u];
+        *(f16x4*)(ep + (32 * i + l32) * 128 + (((4 * j + q) ^ (l32 & 7)) << 4) + 8 * hf) = h;
       }
-      PT_WAVE_LDS_FENCE();
+  PT_WAVE_LDS_FENCE();
+  const int r = lane & 15, oct = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int c0 = 0; c0 < 64; c0 += 16) {
+      pt_u32x4 v;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int row = 32 * i + 8 * oct + 4 * k + (r >> 2), chunk = ((c0 >> 3) + ((r & 3) >> 1)) ^ (row & 7);
+        const pt_u32x2 x = __builtin_bit_cast(
+            pt_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(ep + row * 128 + chunk * 16 + (r & 1) * 8)));
+        v[2 * k] = x[0];
+        v[2 * k + 1] = x[1];
+      }
+      sink(c0 + r, 32 * i + 8 * oct, v);
     }
+  PT_WAVE_LDS_FENCE();
+}
+
+__device__ __forceinline__ uint16_t pt_bits(half_t, float v) { return __builtin_bit_cast(uint16_t, (half_t)v); }
+__device__ __forceinline__ uint16_t pt_bits(bfloat, float v) { return __builtin_bit_cast(uint16_t, (bfloat)v); }
+template <typename T>
+__device__ __forceinline__ pt_u32x4 pt_pack8(const float (&v)[8]) {
+  pt_u32x4 r;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) r[u] = (uint32_t)pt_bits(T(), v[2 * u]) | (uint32_t)pt_bits(T(), v[2 * u + 1]) << 16;
+  return r;
 }
 
 // Tile t of nb_m x nb_n: consecutive tiles walk four row tiles for each column tile.
 __device__ __forceinline__ void pt_tile_pos(int t, int nb_m, int nb_n, int& tm, int& tn) {
-  constexpr int G = 4;
+#ifndef PT_G
+#define PT_G 4
+#endif
+  constexpr int G = PT_G;
   const int grp = t / (G * nb_n), r = t - grp * G * nb_n, gm = min(G, nb_m - grp * G);
   tm = grp * G + r % gm;
   tn = r / gm;
@@ -295,8 +359,15 @@ __device__ __forceinline__ void pt_tile_triangle(int t, int& tm, int& tn) {
 // Work item of this block of a launch of `items` (grid: a multiple of 8 that covers them): block b runs on XCD b % 8, and an
 // XCD takes a contiguous run of items, whose operands its L2 then holds.  -1: none.
 __device__ __forceinline__ int pt_item(int items) {
+#ifdef PT_MAP
+  const int b = (int)blockIdx.x, x = b & 7, r = b >> 3, full = items / 256 * 32;
+  if (r < full) return (r >> 5) * 256 + x * 32 + (r & 31);
+  const int rem = items % 256, per = (rem + 7) >> 3, it = items - rem + x * per + (r - full);
+  return r - full < per && it < items ? it : -1;
+#else
   const int per = (items + 7) >> 3, b = (int)blockIdx.x, it = (b & 7) * per + (b >> 3);
   return (b >> 3) < per && it < items ? it : -1;
+#endif
 }
 inline unsigned pt_grid(int items) { return 8u * (unsigned)((items + 7) / 8); }
 

@@ -26,13 +26,6 @@ namespace {
 using PtBig = PtShape<2, 4, 4, 2>;  // 256 x 256, 8 waves of 128 x 64, a CU to itself (160 KB of LDS)
 using PtMid = PtShape<2, 2, 2, 2>;  // 128 x 128, 4 waves of 64 x 64, two blocks on a CU
 
-#define PT_SHARED(S)                                                  \
-  __shared__ __attribute__((aligned(16))) char la0[S::rows * 128];    \
-  __shared__ __attribute__((aligned(16))) char lw0[S::cols * 128];    \
-  __shared__ __attribute__((aligned(16))) char la1[S::rows * 128];    \
-  __shared__ __attribute__((aligned(16))) char lw1[S::cols * 128];    \
-  __shared__ __attribute__((aligned(16))) char lep[S::waves * 4096];
-
 constexpr int kPart = 64;  // columns of a part
 
 __device__ __forceinline__ uint32_t order_key(float v) {  // larger for larger values, -0 as +0, NaN below all
@@ -52,18 +45,20 @@ struct StatsArgs {
   float *pmax, *ps0, *ps1;  // [part][T]
   float* ztgt;              // [T], the target's logit
   float* logits;            // [T][ldl] or null
-  int ldl;
+  int ldl, tile0, tiles_n;  // column tiles of this launch
+  const float* thr;         // [T] or null: only parts whose maximum is not below their row's are stored
 };
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
   PT_SHARED(S)
   constexpr int MT = S::MT;
-  const int nb_m = (a.T + S::rows - 1) / S::rows, nb_n = (a.V + S::cols - 1) / S::cols;
-  const int item = pt_item(nb_m * nb_n);
+  const int nb_m = (a.T + S::rows - 1) / S::rows;
+  const int item = pt_item(nb_m * a.tiles_n);
   if (item < 0) return;
   int tm, tn;
-  pt_tile_pos(item, nb_m, nb_n, tm, tn);
+  pt_tile_pos(item, nb_m, a.tiles_n, tm, tn);
+  tn += a.tile0;
   pt_f32x16 acc[2][MT];
   pt_product<T, false, false, S>(a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, la0, lw0, la1, lw1, acc);
   int lane = threadIdx.x & 63;
@@ -72,62 +67,81 @@ __global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
   if (col0 >= a.V) return;
   const int part = col0 / kPart;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int row = row0 + 32 * i + l32;
-    const bool in = row < a.T;
-    const int tcol = in ? a.targets[row] - col0 : -1;  // (an absent target is negative)
-    int lim = a.V - col0;  // columns of this wave that exist (opaque: 32 masks would otherwise be held in registers)
+  const float c2 = a.inv_t * 1.44269504088896341f;
+  // the sums of a part; `all`: its 64 columns exist (without it, 32 masks would be held in registers)
+  auto sums = [&](auto all) {
+    constexpr bool ALL = decltype(all)::value;
+    int lim = a.V - col0;
     asm volatile("" : "+s"(lim));
-    float m = -INFINITY, zt = 0.f;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int i = 0; i < MT; ++i) {
+      const int row = row0 + 32 * i + l32;
+      const bool in = row < a.T;
+      float m = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int col = pt_col(j, e, hf);
-        const float v = acc[j][i][e];
-        zt = col == tcol ? v : zt;
-        m = fmaxf(m, col < lim ? v : -INFINITY);
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, ALL || pt_col(j, e, hf) < lim ? acc[j][i][e] : -INFINITY);
+      m = half_max(m);
+      float s0 = 0.f, s1 = 0.f;
+      if (m > -INFINITY) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float t = fmaxf((acc[j][i][e] - m) * c2, -1e30f);  // (0 times -infinity)
+            float x = __builtin_amdgcn_exp2f(t);
+            if (acc[j][i][e] != acc[j][i][e]) x = acc[j][i][e];      // (the maximum passes over NaN)
+            if (!ALL) x = pt_col(j, e, hf) < lim ? x : 0.f;
+            s0 += x;
+            s1 = fmaf(x, t, s1);
+          }
+      } else {  // -infinity alone, or NaN
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (pt_col(j, e, hf) < lim && acc[j][i][e] != acc[j][i][e]) s0 = acc[j][i][e];
       }
-    m = half_max(m);
-    float s0 = 0.f, s1 = 0.f;
-    if (m > -INFINITY) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float t = (acc[j][i][e] - m) * a.inv_t;
-          float x = __expf(t);
-          x = pt_col(j, e, hf) < lim ? x : 0.f;
-          s0 += x;
-          s1 += x != 0.f ? x * t : 0.f;  // (0 times -infinity)
-        }
-    } else {  // -infinity alone, or NaN (which the maximum passes over)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (pt_col(j, e, hf) < lim && acc[j][i][e] != acc[j][i][e]) s0 = acc[j][i][e];
-    }
-    s0 = half_sum(s0);
-    s1 = half_sum(s1);
-    if (in) {
-      if (hf == 0) {
+      s0 = half_sum(s0);
+      s1 = half_sum(s1);
+      if (in && hf == 0) {
         const size_t at = (size_t)part * a.T + row;
         a.pmax[at] = m;
         a.ps0[at] = s0;
-        a.ps1[at] = s1;
+        a.ps1[at] = s1 * 0.69314718055994531f;
       }
-      if (tcol >= 0 && tcol < 64 && ((tcol >> 2) & 1) == hf) a.ztgt[row] = zt;
+      if (a.thr) {  // few rows keep their part: straight from the accumulators
+        const bool keep = in && !(m < a.thr[min(row, a.T - 1)]);
+        if (__ballot(keep)) {
+          float* const o = a.logits + (size_t)row * a.ldl + col0 + 4 * hf;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (keep)
+                *(pt_f32x4*)(o + 32 * j + 8 * q) =
+                    pt_f32x4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
+        }
+      }
+      // the target's logit, where one of the wave's rows has it here
+      const int tcol = in ? a.targets[row] - col0 : -1;  // (an absent target is negative)
+      if (__ballot((unsigned)tcol < 64u)) {
+        float zt = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) zt = pt_col(j, e, hf) == tcol ? acc[j][i][e] : zt;
+        if ((unsigned)tcol < 64u && ((tcol >> 2) & 1) == hf) a.ztgt[row] = zt;
+      }
     }
-  }
-  if (a.logits) {  // (columns up to the row stride, a multiple of 64, exist)
-    char* const ep = lep + wave * 4096;
-    pt_hand_out_32<MT, 2>(
-        ep, lane, [&](int j, int i, int e) { return acc[j][i][e]; },
-        [&](int r, int c, pt_f32x4 v) {
-          if (row0 + r < a.T) *(pt_f32x4*)(a.logits + (size_t)(row0 + r) * a.ldl + col0 + c) = v;
-        });
+  };
+  if (a.V - col0 >= 64) sums(std::true_type{});
+  else sums(std::false_type{});
+  if (a.logits && !a.thr) {  // (columns up to the row stride, a multiple of 64, exist)
+    pt_hand_out<4, MT>(pt_wave_lds<S>(la0, lw0, la1, lw1, wave), lane, acc, PtNothing(), [&](int r, int c, pt_f32x4 v, int) {
+      if (row0 + r < a.T) *(pt_f32x4*)(a.logits + (size_t)(row0 + r) * a.ldl + col0 + c) = v;
+    });
   }
 }
 
@@ -152,23 +166,21 @@ __device__ __forceinline__ Stat stat_merge(Stat a, Stat b, float inv_t) {
   return r;
 }
 
+// 4-byte words of LDS of a wave that looks for alternatives
+__host__ __device__ constexpr int finish_words(int top) { return top * (kPart + 2) < 160 ? 160 : top * (kPart + 2); }
+
 struct FinishArgs {
   const float *pmax, *ps0, *ps1, *ztgt, *logits;
   const int32_t* targets;
-  int T, V, parts, ldl, top, rows;  // rows per block: 1, 4 or 16
+  int T, V, parts, ldl, top;
   float inv_t;
   float *logprob, *entropy, *lse;
   int32_t* top_ids;
   float* top_logprob;
 };
 
-__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
-  auto step = [&](auto o) {
-    constexpr int O = decltype(o)::value;
-    const uint32_t lo = (uint32_t)lane_xor<O>((int)(uint32_t)v), hi = (uint32_t)lane_xor<O>((int)(uint32_t)(v >> 32));
-    const uint64_t x = (uint64_t)hi << 32 | lo;
-    v = x > v ? x : v;
-  };
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  auto step = [&](auto o) { v = max(v, (uint32_t)lane_xor<decltype(o)::value>((int)v)); };
   step(std::integral_constant<int, 32>{});
   step(std::integral_constant<int, 16>{});
   step(std::integral_constant<int, 8>{});
@@ -178,91 +190,262 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
   return v;
 }
 
-// Block: `rows` rows, 256 / rows threads to each for the sums; then a wave per row for the alternatives.
-// LDS: the rows' part maxima [parts][rows + 1] (with alternatives), each wave's candidates [top * 64] and parts [top].
+// The k first of n keys in LDS in the order (key descending, place ascending), one by one: lane l has the places l, l + 64, ...; every
+// lane keeps the first of its own that is left, and the lane whose key is taken looks for its next (eight loads at a time
+// under way: a loop that waits for each is most of the kernel).  take(rank, key, place) is called by all lanes.
+template <typename F>
+__device__ __forceinline__ void wave_select(const uint32_t* keys, int n, int k, int lane, F take) {
+  uint32_t bk = 0, bi = ~0u;
+  auto look = [&](uint32_t lk, uint32_t li) {  // this lane's first behind (lk, li)
+    bk = 0;
+    bi = ~0u;
+    for (int i0 = lane; i0 < n; i0 += 512) {
+      uint32_t x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = keys[min(i0 + 64 * u, n - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const uint32_t i = i0 + 64 * u;
+        const bool behind = i < (uint32_t)n && (x[u] < lk || (x[u] == lk && i > li));
+        if (behind && (x[u] > bk || bi == ~0u)) bk = x[u], bi = i;
+      }
+    }
+  };
+  look(~0u, 0);  // (no key is ~0: that would be a NaN)
+  for (int r = 0; r < k; ++r) {
+    const uint32_t top = wave_max_u32(bk);
+    const uint32_t first = ~wave_max_u32(bk == top ? ~bi : 0u);
+    take(r, top, first);
+    if (bi == first) look(top, first);
+  }
+}
+
+// A value that at least k of the lanes' items are not below, and few more: the k-th largest of the lanes' largest (k <= 64).
+__device__ __forceinline__ uint32_t wave_bound(uint32_t largest, int k) {
+  int above = 0;
+#pragma unroll
+  for (int l = 0; l < 64; ++l) above += (uint32_t)__builtin_amdgcn_readlane((int)largest, l) > largest ? 1 : 0;
+  return ~wave_max_u32(above < k ? ~largest : 0u);
+}
+__device__ __forceinline__ int lanes_below(uint64_t mask) {  // set bits below this lane's
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+}
+
+constexpr int kQuickTop = 32, kQuickParts = 32;
+
+// The alternatives of one row by a wave, quickly: the parts whose maximum reaches a bound that k part maxima reach; of their
+// logits those that reach a bound that k of them reach; and the ranks of these, at most 64, by comparing all with all.
+// False, with nothing written, where ties or an odd spread leave more than fit.
+template <int NB>
+__device__ __forceinline__ bool rank_logits(const float* logits, int V, const int* sel, int parts, int top, int lane, uint32_t* keep_key,
+                                            int* keep_col, float inv_t, float lse, int32_t* ids, float* lps) {
+  uint32_t x[NB], largest = 0;
+  int col[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    col[j] = sel[min(j, parts - 1)] * kPart + lane;
+    x[j] = __float_as_uint(logits[min(col[j], V - 1)]);
+  }
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const bool in = j < parts && col[j] < V;
+    x[j] = in ? order_key(__uint_as_float(x[j])) : 0u;
+    if (!in) col[j] = -1;
+    largest = max(largest, x[j]);
+  }
+  const uint32_t bound = wave_bound(largest, top);
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const bool keep = col[j] >= 0 && x[j] >= bound;
+    const uint64_t who = __ballot(keep);
+    const int at = n + lanes_below(who);
+    if (keep && at < 64) {
+      keep_key[at] = x[j];
+      keep_col[at] = col[j];
+    }
+    n += __popcll(who);
+  }
+  if (n > 64) return false;
+  PT_WAVE_LDS_FENCE();
+  const uint32_t key = keep_key[min(lane, n - 1)];
+  const int c = keep_col[min(lane, n - 1)];
+  int rank = 0;
+  for (int l = 0; l < n; ++l) {
+    const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key, l);
+    rank += k > key || (k == key && __builtin_amdgcn_readlane(c, l) < c) ? 1 : 0;
+  }
+  if (lane < n && rank < top) {
+    ids[rank] = c;
+    lps[rank] = order_value(key) * inv_t - lse;
+  }
+  return true;
+}
+
+// The places (ascending, up to `most`) of the keys that reach the bound of k of them; returns how many reach it.
+__device__ __forceinline__ int bounded_places(const uint32_t* keys, int n, int k, int most, int lane, int* places) {
+  uint32_t largest = 0;
+  for (int i0 = lane; i0 < n; i0 += 512)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const uint32_t x = keys[min(i0 + 64 * u, n - 1)];
+      largest = max(largest, i0 + 64 * u < n ? x : 0u);
+    }
+  const uint32_t bound = wave_bound(largest, k);
+  int found = 0;
+  for (int i0 = 0; i0 < n; i0 += 512) {
+    uint32_t x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = keys[min(i0 + 64 * u + lane, n - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + 64 * u + lane;
+      const bool keep = i < n && x[u] >= bound;
+      const uint64_t who = __ballot(keep);
+      const int at = found + lanes_below(who);
+      if (keep && at < most) places[at] = i;
+      found += __popcll(who);
+    }
+  }
+  return found;
+}
+
+// Block: R rows, 256 / R threads to each for the sums; then a wave per row for the alternatives.
+// LDS: the keys of the rows' part maxima [R][parts | 1] (with alternatives), then of each wave its candidates' [top * 64] and the
+// parts [top], as chosen and by id, or (the quick way) the parts [32] and the keys and ids of what is ranked [64].
+template <int R>
 __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];
-  __shared__ float sh[3][256];
+  __shared__ float sh[3][4][16];
   __shared__ float row_lse[16];
-  const int tid = threadIdx.x, R = a.rows, G = 256 / R, r = tid % R, g = tid / R;
+  constexpr int G = 256 / R;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = tid % R, g = tid / R, P = a.parts | 1;
   const int row = blockIdx.x * R + r;
   const bool in = row < a.T;
-  float* const pm = (float*)dyn;
+  uint32_t* const pm = (uint32_t*)dyn;
   Stat s = {-INFINITY, 0.f, 0.f};
   if (in) {
     for (int p = g; p < a.parts; p += G) {
       const size_t at = (size_t)p * a.T + row;
       const Stat x = {a.pmax[at], a.ps0[at], a.ps1[at]};
-      if (a.top) pm[p * (R + 1) + r] = x.m;
+      if (a.top) pm[r * P + p] = order_key(x.m);
       s = stat_merge(s, x, a.inv_t);
     }
   }
-  for (int half = G / 2; half; half /= 2) {  // a fixed tree over the row's threads
-    sh[0][tid] = s.m;
-    sh[1][tid] = s.s0;
-    sh[2][tid] = s.s1;
+  // over the row's threads: the maximum, then the sums brought to it, in a fixed order
+  auto over = [&](float v, auto op, int k) {
+    if (R <= 1) v = op(v, lane_xor<1>(v));
+    if (R <= 2) v = op(v, lane_xor<2>(v));
+    if (R <= 4) v = op(v, lane_xor<4>(v));
+    if (R <= 8) v = op(v, lane_xor<8>(v));
+    v = op(v, lane_xor<16>(v));
+    v = op(v, lane_xor<32>(v));
+    if (lane < R) sh[k][wave][lane] = v;
     __syncthreads();
-    if (g < half) s = stat_merge(s, Stat{sh[0][tid + half * R], sh[1][tid + half * R], sh[2][tid + half * R]}, a.inv_t);
-    __syncthreads();
-  }
+    return op(op(sh[k][0][r], sh[k][1][r]), op(sh[k][2][r], sh[k][3][r]));
+  };
+  const float m = over(s.m, [](float x, float y) { return fmaxf(x, y); }, 0);
+  s = stat_merge(s, Stat{m, 0.f, 0.f}, a.inv_t);
+  s.s0 = over(s.s0, [](float x, float y) { return x + y; }, 1);
+  s.s1 = over(s.s1, [](float x, float y) { return x + y; }, 2);
   if (g == 0 && in) {
-    const float ls = logf(s.s0), l = s.m * a.inv_t + ls;
+    const float ls = logf(s.s0), l = m * a.inv_t + ls;
     row_lse[r] = l;
     a.lse[row] = l;
     a.entropy[row] = ls - s.s1 / s.s0;
     const int y = a.targets[row];
-    a.logprob[row] = y >= 0 && y < a.V ? (a.ztgt[row] - s.m) * a.inv_t - ls : 0.f;
+    a.logprob[row] = y >= 0 && y < a.V ? (a.ztgt[row] - m) * a.inv_t - ls : 0.f;
   }
   if (!a.top) return;
   __syncthreads();
-  const int lane = tid & 63, wave = tid >> 6, kp = min(a.top, a.parts);
-  float* const cand = pm + a.parts * (R + 1) + wave * (a.top * (kPart + 1));
-  int* const sel = (int*)(cand + a.top * kPart);
+  const int kp = min(a.top, a.parts);
+  uint32_t* const cand = pm + R * P + wave * finish_words(a.top);
+  int *const chosen = (int*)(cand + a.top * kPart), *const sel = chosen + a.top;
   for (int q = wave; q < R; q += 4) {
     const int t = blockIdx.x * R + q;
     if (t >= a.T) break;
-    uint64_t last = ~0ull;
-    for (int k = 0; k < kp; ++k) {
-      uint64_t best = 0;
-      for (int p = lane; p < a.parts; p += 64) {
-        const uint64_t x = (uint64_t)order_key(pm[p * (R + 1) + q]) << 32 | (0xFFFFFFFFu - (uint32_t)p);
-        if (x < last && x > best) best = x;
-      }
-      last = wave_max_u64(best);
-      if (lane == 0) sel[k] = (int)(0xFFFFFFFFu - (uint32_t)last);
+    if (a.top <= kQuickTop) {
+      int *const places = (int*)cand, *const cols = places + kQuickParts + 64;
+      uint32_t* const keys = cand + kQuickParts;
+      const int n = bounded_places(pm + q * P, a.parts, kp, kQuickParts, lane, places);
+      PT_WAVE_LDS_FENCE();
+      const float* const row_logits = a.logits + (size_t)t * a.ldl;
+      int32_t* const ids = a.top_ids + (size_t)t * a.top;
+      float* const lps = a.top_logprob + (size_t)t * a.top;
+      bool done = false;
+      if (n <= 12) done = rank_logits<12>(row_logits, a.V, places, n, a.top, lane, keys, cols, a.inv_t, row_lse[q], ids, lps);
+      else if (n <= kQuickParts) done = rank_logits<kQuickParts>(row_logits, a.V, places, n, a.top, lane, keys, cols, a.inv_t, row_lse[q], ids, lps);
+      PT_WAVE_LDS_FENCE();
+      if (done) continue;
+    }
+    wave_select(pm + q * P, a.parts, kp, lane, [&](int k, uint32_t, uint32_t i) {
+      if (lane == 0) chosen[k] = (int)i;
+    });
+    PT_WAVE_LDS_FENCE();
+    if (lane < kp) {  // in the order of their ids, so that a candidate's place orders as its id does
+      const int mine = chosen[lane];
+      int rank = 0;
+      for (int k = 0; k < kp; ++k) rank += chosen[k] < mine;
+      sel[rank] = mine;
     }
     PT_WAVE_LDS_FENCE();
-    for (int k = 0; k < kp; ++k) {
+    for (int k = 0; k < kp; ++k) {  // (ids past the vocabulary come last and are not reached)
       const int col = sel[k] * kPart + lane;
-      cand[k * kPart + lane] = col < a.V ? a.logits[(size_t)t * a.ldl + col] : 0.f;
+      cand[k * kPart + lane] = col < a.V ? order_key(a.logits[(size_t)t * a.ldl + col]) : 0u;
     }
+    PT_WAVE_LDS_FENCE();
     const float lse = row_lse[q];
-    last = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-      uint64_t best = 0;
-      for (int j = 0; j < kp; ++j) {
-        const int col = sel[j] * kPart + lane;
-        const uint64_t x = (uint64_t)order_key(cand[j * kPart + lane]) << 32 | (0xFFFFFFFFu - (uint32_t)col);
-        if (col < a.V && x < last && x > best) best = x;
-      }
-      last = wave_max_u64(best);
+    wave_select(cand, kp * kPart, a.top, lane, [&](int k, uint32_t key, uint32_t i) {
       if (lane == 0) {
-        a.top_ids[(size_t)t * a.top + k] = (int)(0xFFFFFFFFu - (uint32_t)last);
-        a.top_logprob[(size_t)t * a.top + k] = order_value((uint32_t)(last >> 32)) * a.inv_t - lse;
+        a.top_ids[(size_t)t * a.top + k] = sel[i >> 6] * kPart + (int)(i & 63);
+        a.top_logprob[(size_t)t * a.top + k] = order_value(key) * a.inv_t - lse;
       }
-    }
+    });
     PT_WAVE_LDS_FENCE();
   }
 }
 
-// dst [grid][ldd] = src [rows][cols] (row stride lds), zero beyond either
+// thr[row] = a bound that `top` of the row's first `parts` maxima reach: no part below it can hold one of the row's top entries.
+__global__ void __launch_bounds__(256) stats_threshold_kernel(const float* __restrict__ pmax, int T, int parts, int top, float* __restrict__ thr) {
+  extern __shared__ __attribute__((aligned(16))) char dyn[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = parts | 1;
+  uint32_t* const pm = (uint32_t*)dyn;
+  for (int i = tid; i < 16 * parts; i += 256) {
+    const int row = blockIdx.x * 16 + (i & 15);
+    if (row < T) pm[(i & 15) * P + (i >> 4)] = order_key(pmax[(size_t)(i >> 4) * T + row]);
+  }
+  __syncthreads();
+  for (int q = wave; q < 16; q += 4) {
+    const int row = blockIdx.x * 16 + q;
+    if (row >= T) break;
+    uint32_t largest = 0;
+    for (int i = lane; i < parts; i += 64) largest = max(largest, pm[q * P + i]);
+    const uint32_t bound = wave_bound(largest, top);
+    if (lane == 0) thr[row] = bound ? order_value(bound) : -INFINITY;
+  }
+}
+
+// dst [rows_to][ldd] = src [rows][cols] (row stride lds), zero beyond either; 16 bytes of dst a thread.  Rows of src may start at
+// any element: its loads need no more alignment than that.
 template <typename T>
 __global__ void __launch_bounds__(256)
-    pack_rows_kernel(const T* __restrict__ src, size_t lds, int rows, int cols, T* __restrict__ dst, int ldd) {
-  const T* const s = src + (size_t)blockIdx.x * lds;
-  T* const o = dst + (size_t)blockIdx.x * ldd;
-  const int n = (int)blockIdx.x < rows ? cols : 0;
-  for (int c = threadIdx.x; c < ldd; c += 256) o[c] = c < n ? s[c] : (T)0.f;
+    pack_rows_kernel(const T* __restrict__ src, size_t lds, int rows, int cols, T* __restrict__ dst, int ldd, int rows_to) {
+  constexpr int E = 16 / (int)sizeof(T);
+  typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t loose;
+  const int per_row = ldd / E;
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
+  const int c = (int)(i - row * per_row) * E;
+  if (row >= (size_t)rows_to) return;
+  const T* const s = src + row * lds + c;
+  T v[E];
+  if (row < (size_t)rows && c + E <= cols) {
+    const loose x = *(const loose*)s;
+    __builtin_memcpy(v, &x, 16);
+  } else {
+#pragma unroll
+    for (int u = 0; u < E; ++u) v[u] = row < (size_t)rows && c + u < cols ? s[u] : (T)0.f;
+  }
+  __builtin_memcpy(__builtin_assume_aligned(dst + row * ldd + c, 16), v, 16);
 }
 
 // scale[0] = the power of two that brings the largest |dz| a row could have (|g| + 14 |e|, |log p + H| p being less) to 2^11 .. 2^12, well
@@ -301,9 +484,6 @@ struct DzArgs {
   int ldz, rows;
 };
 
-__device__ __forceinline__ uint16_t bits_of(half_t, float v) { return __builtin_bit_cast(uint16_t, (half_t)v); }
-__device__ __forceinline__ uint16_t bits_of(bfloat, float v) { return __builtin_bit_cast(uint16_t, (bfloat)v); }
-
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, 2) dz_kernel(DzArgs a) {
   PT_SHARED(S)
@@ -319,42 +499,49 @@ __global__ void __launch_bounds__(64 * S::waves, 2) dz_kernel(DzArgs a) {
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
-  char* const ep = lep + wave * 4096;
+  if (row0 >= a.rows || col0 >= a.ldz) return;
   const float s = (a.scale ? a.scale[0] : 1.f) * a.inv_t;
-  int lim = a.V - col0;
-  asm volatile("" : "+s"(lim));
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const bool in = row0 + 32 * i + l32 < a.T;
     const int row = min(row0 + 32 * i + l32, a.T - 1);
     const int t = a.targets[row], y = t < a.V ? t : -1;
     const float g = y >= 0 ? a.g[row] * s : 0.f, e = a.e ? a.e[row] * s : 0.f;
     const float lse = a.lse[row], H = a.entropy[row];  // (H: anything without e)
-    const int tcol = y - col0;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
-        const int col = pt_col(j, x, hf);
+        // (a finite log p: 0 times infinity)
         const float logp = fmaf(acc[j][i][x], a.inv_t, -lse), p = __expf(logp);
-        float v = p != 0.f ? -p * (g + e * (logp + H)) : 0.f;  // (0 times infinity)
-        if (logp != logp) v = logp;
-        v += y >= 0 && col == tcol ? g : 0.f;
-        acc[j][i][x] = in && col < lim ? v : 0.f;
+        acc[j][i][x] = -p * (g + e * (fmaxf(logp, -1e30f) + H));
       }
+    const int tcol = y >= 0 ? y - col0 : -1;
+    if (__ballot((unsigned)tcol < 64u)) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) acc[j][i][x] += pt_col(j, x, hf) == tcol ? g : 0.f;
+    }
   }
+  const bool edge = a.V - col0 < 64 || row0 + 32 * MT > a.T;  // some of the wave's columns or rows do not exist: zeros
+  char* const ep = pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
+  T* const dz = (T*)a.dz + (size_t)row0 * a.ldz + col0;
   if constexpr (sizeof(T) == 2) {
-    pt_hand_out_16<MT>(
-        ep, lane, [&](int j, int i, int e) { return bits_of(T(), acc[j][i][e]); },
-        [&](int r, int c, pt_u32x4 v) {
-          if (row0 + r < a.rows && col0 + c < a.ldz) *(pt_u32x4*)((T*)a.dz + (size_t)(row0 + r) * a.ldz + col0 + c) = v;
-        });
+    pt_hand_out<8, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, float(&v)[8], int) {
+      if (edge) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = row0 + r < a.T && col0 + c + u < a.V ? v[u] : 0.f;
+      }
+      if (row0 + r < a.rows) *(pt_u32x4*)(dz + (size_t)r * a.ldz + c) = pt_pack8<T>(v);
+    });
   } else {
-    pt_hand_out_32<MT, 2>(
-        ep, lane, [&](int j, int i, int e) { return acc[j][i][e]; },
-        [&](int r, int c, pt_f32x4 v) {
-          if (row0 + r < a.rows && col0 + c < a.ldz) *(pt_f32x4*)((float*)a.dz + (size_t)(row0 + r) * a.ldz + col0 + c) = v;
-        });
+    pt_hand_out<4, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, pt_f32x4 v, int) {
+      if (edge) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = row0 + r < a.T && col0 + c + u < a.V ? v[u] : 0.f;
+      }
+      if (row0 + r < a.rows) *(pt_f32x4*)(dz + (size_t)r * a.ldz + c) = v;
+    });
   }
 }
 
@@ -407,40 +594,36 @@ __global__ void __launch_bounds__(64 * S::waves, 2) out_kernel(OutArgs a) {
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
-  char* const ep = lep + wave * 4096;
+  char* const ep = pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
   if (a.slices > 1) {
     float* const o = a.slab + (size_t)z * a.M * a.lds;
-    pt_hand_out_32<MT, 2>(
-        ep, lane, [&](int j, int i, int e) { return acc[j][i][e]; },
-        [&](int r, int c, pt_f32x4 v) {
-          if (row0 + r < a.M && col0 + c < a.lds) *(pt_f32x4*)(o + (size_t)(row0 + r) * a.lds + col0 + c) = v;
-        });
+    pt_hand_out<4, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, pt_f32x4 v, int) {
+      if (row0 + r < a.M && col0 + c < a.lds) *(pt_f32x4*)(o + (size_t)(row0 + r) * a.lds + col0 + c) = v;
+    });
     return;
   }
   const float s = a.scale ? a.scale[1] : 1.f;
   const bool vec = ((uintptr_t)a.out & 15) == 0 && a.ldo % (a.f32 ? 4 : 8) == 0;
-  if (sizeof(T) == 2 && !a.f32 && vec) {
+  if (sizeof(T) == 2 && !a.f32) {
     if constexpr (sizeof(T) == 2) {
-      pt_hand_out_16<MT>(
-          ep, lane, [&](int j, int i, int e) { return bits_of(T(), acc[j][i][e] * s); },
-          [&](int r, int c, pt_u32x4 v) {
-            if (row0 + r >= a.M) return;
-            uint16_t* const o = (uint16_t*)a.out + (size_t)(row0 + r) * a.ldo + col0 + c;
-            if (col0 + c + 8 <= a.N) {
-              *(pt_u32x4*)o = v;
-            } else {
+      pt_hand_out<8, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, float(&v)[8], int) {
+        if (row0 + r >= a.M) return;
+        T* const o = (T*)a.out + (size_t)(row0 + r) * a.ldo + col0 + c;
 #pragma unroll
-              for (int u = 0; u < 8; ++u)
-                if (col0 + c + u < a.N) o[u] = (uint16_t)(v[u >> 1] >> (16 * (u & 1)));
-            }
-          });
+        for (int u = 0; u < 8; ++u) v[u] *= s;
+        if (vec && col0 + c + 8 <= a.N) {
+          *(pt_u32x4*)o = pt_pack8<T>(v);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if (col0 + c + u < a.N) o[u] = (T)v[u];
+        }
+      });
     }
   } else {
-    pt_hand_out_32<MT, 2>(
-        ep, lane, [&](int j, int i, int e) { return acc[j][i][e] * s; },
-        [&](int r, int c, pt_f32x4 v) {
-          if (row0 + r < a.M) out_store<T>(a, row0 + r, col0 + c, v, vec);
-        });
+    pt_hand_out<4, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, pt_f32x4 v, int) {
+      if (row0 + r < a.M) out_store<T>(a, row0 + r, col0 + c, v * s, vec);
+    });
   }
 }
 
@@ -489,12 +672,12 @@ int stage_of(int dtype) { return 128 / (int)elem_size(dtype); }  // k of a stage
 int whole(int n, int stage) { return (n + stage - 1) / stage * stage; }
 int padded(int n) { return whole(n, 64); }
 
-constexpr int kLogitRows = 4096;   // rows of stored logits at a time
+constexpr int kLogitRows = 16384;  // rows of stored logits at a time
 constexpr int kGradRows = 16384;   // rows of dz at a time
 
 int equal_chunk(int T, int most) {  // rows of a chunk: as few chunks as there must be, of about the same size
   const int n = (T + most - 1) / most;
-  return std::min(T, ((T + n - 1) / n + 127) & ~127);
+  return std::min(T, ((T + n - 1) / n + 255) & ~255);
 }
 
 template <typename F>
@@ -516,12 +699,31 @@ Operand packed(Bump& ws, const TokenRows& m, int rows, int d, int dtype, hipStre
   if (to)
     by_type(dtype, [&](auto t) {
       using T = decltype(t);
-      hipLaunchKernelGGL(pack_rows_kernel<T>, dim3(rows_to), dim3(256), 0, s, (const T*)m.p, (size_t)m.ld, rows, d, (T*)to, ldd);
+      const size_t chunks = (size_t)rows_to * ldd / (16 / sizeof(T));
+      hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const T*)m.p, (size_t)m.ld, rows, d,
+                         (T*)to, ldd, rows_to);
     });
   return {to, (uint32_t)ldd};
 }
 
-size_t finish_lds(int parts, int rows, int top) { return top ? ((size_t)parts * (rows + 1) + (size_t)std::min(rows, 4) * top * (kPart + 1)) * 4 : 0; }
+size_t finish_lds(int parts, int rows, int top) {
+  return top ? ((size_t)rows * (parts | 1) + (size_t)std::min(rows, 4) * finish_words(top)) * 4 : 0;
+}
+
+// Column tiles whose logits are stored whole, so that their part maxima bound what the others need to store: an eighth of the
+// vocabulary or so, a count that leaves both launches rounds of 256 tiles as full as any does; 0: one launch that stores all.  (13,568
+// rows of 50,304 entries, eight alternatives: all stored 3.33 ms, this way 3.0, no alternatives 2.74.)
+int sample_tiles(int T, int V, int top) {
+  const int nb_m = (T + 255) / 256, nb_n = (V + 255) / 256;
+  if (!top || nb_m * nb_n < 2048 || nb_n < 32) return 0;
+  int best = 0, best_r = INT_MAX;
+  for (int n = nb_n / 6; n >= nb_n / 12; --n) {
+    if (4 * n < 4 * top) break;
+    const int r = (nb_m * n + 255) / 256 + (nb_m * (nb_n - n) + 255) / 256;
+    if (r < best_r) best = n, best_r = r;
+  }
+  return best;
+}
 
 }  // namespace
 
@@ -537,10 +739,9 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
   StatsArgs k;
   float* const part = ws.take<float>((size_t)3 * parts * rows);
   float* const ztgt = ws.take<float>(rows);
+  float* const thr = ws.take<float>(a.top ? rows : 0);
   float* const logits = a.top ? ws.take<float>((size_t)rows * padded(a.V)) : nullptr;
   if (!workspace) return ws.off;
-  int R = rows >= 4096 ? 16 : rows >= 1024 ? 4 : 1;  // rows of a finishing block: many share the lines of the parts' sums
-  while (R > 1 && finish_lds(parts, R, a.top) > 60 * 1024) R /= 4;
   for (int t0 = 0; t0 < a.T; t0 += rows) {
     const int n = std::min(rows, a.T - t0);
     k.h = (const char*)h.p + (size_t)t0 * h.ld * elem_size(a.dtype);
@@ -558,17 +759,38 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
     k.ztgt = ztgt;
     k.logits = logits;
     k.ldl = padded(a.V);
+    k.thr = nullptr;
     by_type(a.dtype, [&](auto t) {
       using T = decltype(t);
-      if (big_tiles(n, a.V))
-        hipLaunchKernelGGL((stats_kernel<T, PtBig>), dim3(pt_grid(tiles(n, a.V, 256, 256))), dim3(512), 0, s, k);
-      else
-        hipLaunchKernelGGL((stats_kernel<T, PtMid>), dim3(pt_grid(tiles(n, a.V, 128, 128))), dim3(256), 0, s, k);
+      auto run = [&](auto shape, int from, int to) {
+        using S = decltype(shape);
+        k.tile0 = from;
+        k.tiles_n = to - from;
+        hipLaunchKernelGGL((stats_kernel<T, S>), dim3(pt_grid(((n + S::rows - 1) / S::rows) * (to - from))), dim3(64 * S::waves), 0, s, k);
+      };
+      if (!big_tiles(n, a.V)) {
+        run(PtMid(), 0, (a.V + 127) / 128);
+      } else if (const int first = sample_tiles(n, a.V, a.top)) {
+        run(PtBig(), 0, first);
+        hipLaunchKernelGGL(stats_threshold_kernel, dim3((n + 15) / 16), dim3(256), 16 * (size_t)(4 * first | 1) * 4, s, k.pmax, n, 4 * first,
+                           a.top, thr);
+        k.thr = thr;
+        run(PtBig(), first, (a.V + 255) / 256);
+      } else {
+        run(PtBig(), 0, (a.V + 255) / 256);
+      }
     });
-    FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, R, a.inv_t,
+    FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, a.inv_t,
                     a.logprob + t0, a.entropy + t0, a.lse + t0, a.top ? a.top_ids + (size_t)t0 * a.top : nullptr,
                     a.top ? a.top_logprob + (size_t)t0 * a.top : nullptr};
-    hipLaunchKernelGGL(stats_finish_kernel, dim3((n + R - 1) / R), dim3(256), finish_lds(parts, R, a.top), s, f);
+    auto finish = [&](auto r) {
+      constexpr int R = decltype(r)::value;
+      hipLaunchKernelGGL(stats_finish_kernel<R>, dim3((n + R - 1) / R), dim3(256), finish_lds(parts, R, a.top), s, f);
+    };
+    // rows of a finishing block: many share the lines of the parts' sums, few leave no CU idle
+    if (n >= 4096 && finish_lds(parts, 8, a.top) <= 60 * 1024) finish(std::integral_constant<int, 8>{});
+    else if (n >= 1024 && finish_lds(parts, 4, a.top) <= 60 * 1024) finish(std::integral_constant<int, 4>{});
+    else finish(std::integral_constant<int, 1>{});
     if ((*err = hipGetLastError()) != hipSuccess) return ws.off;
   }
   return ws.off;
