@@ -14,6 +14,7 @@
 // matrix cores run at full rate, and the rounding, half a step of 2^-8 or 2^-11 relative, is that of the results in the same
 // type); dh and dW read it row-major and K-major, W and h as they lie.
 #include <algorithm>
+#include <cmath>
 
 #include "common.h"
 #include "product_tile.h"
@@ -481,18 +482,19 @@ struct DzArgs {
   const float* scale;                  // null: 1
   float inv_t;
   void* dz;  // [rows][ldz], zero from T and V on
-  int ldz, rows;
+  int ldz, rows, tile0, tiles_n;
 };
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, 2) dz_kernel(DzArgs a) {
   PT_SHARED(S)
   constexpr int MT = S::MT;
-  const int nb_m = (a.T + S::rows - 1) / S::rows, nb_n = (a.V + S::cols - 1) / S::cols;
-  const int item = pt_item(nb_m * nb_n);
+  const int nb_m = (a.T + S::rows - 1) / S::rows;
+  const int item = pt_item(nb_m * a.tiles_n);
   if (item < 0) return;
   int tm, tn;
-  pt_tile_pos(item, nb_m, nb_n, tm, tn);
+  pt_tile_pos(item, nb_m, a.tiles_n, tm, tn);
+  tn += a.tile0;
   pt_f32x16 acc[2][MT];
   pt_product<T, false, false, S>(a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, la0, lw0, la1, lw1, acc);
   int lane = threadIdx.x & 63;
@@ -555,7 +557,7 @@ struct OutArgs {
   size_t ldo;
   int f32, add;  // out is float; added to what is there (float only)
   float* slab;   // slices > 1: [slice][M][lds]
-  int lds;
+  int lds, tile0, tiles_n;
 };
 
 template <typename T>
@@ -581,12 +583,14 @@ template <typename T, bool AK, bool WK, typename S>
 __global__ void __launch_bounds__(64 * S::waves, 2) out_kernel(OutArgs a) {
   PT_SHARED(S)
   constexpr int MT = S::MT;
-  const int nb_m = (a.M + S::rows - 1) / S::rows, nb_n = (a.N + S::cols - 1) / S::cols;
+  // (rows are walked as columns are elsewhere: dW has many of them, dh is cut along K)
+  const int nb_m = a.tiles_n, nb_n = (a.N + S::cols - 1) / S::cols;
   const int item = pt_item(nb_m * nb_n * a.slices);
   if (item < 0) return;
   const int z = item / (nb_m * nb_n);
   int tm, tn;
   pt_tile_pos(item - z * nb_m * nb_n, nb_m, nb_n, tm, tn);
+  tm += a.tile0;
   pt_f32x16 acc[2][MT];
   pt_product<T, AK, WK, S>(a.A, a.lda, tm * S::rows, a.M, a.W, a.ldw, tn * S::cols, a.N, z * a.k_slice,
                            min(a.K, (z + 1) * a.k_slice), la0, lw0, la1, lw1, acc);
@@ -652,8 +656,24 @@ __global__ void __launch_bounds__(256) narrow_rows_kernel(const float* __restric
 
 int tiles(int m, int n, int tm, int tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); }
 
-// The larger tile, whose operands are used twice as often, where its tiles fill the chip.
-bool big_tiles(int M, int N) { return tiles(M, N, 256, 256) >= 256; }
+// How a product's columns are cut: `big` column tiles of 256 (256 x 256, a CU each) first, the rest in tiles of 128 (128 x 128, two
+// on a CU).  16-bit types: a round of 256 large tiles takes 1.95 us a stage, one of 512 small ones 1.5 (and of up to 256 1.0), so
+// the large ones make whole rounds and the small ones what is left.  float: the matrix instructions take 16 times as long and
+// nothing else counts: per tile as much as its area.
+int big_columns(int M, int N, int dtype) {
+  const int nb_m = (M + 255) / 256, nb_n = (N + 255) / 256, mid_m = (M + 127) / 128, mid_n = (N + 127) / 128;
+  const double round = dtype == kTokensF32 ? 4.0 : 1.95, small = dtype == kTokensF32 ? 2.0 : 1.5, half = dtype == kTokensF32 ? 1.05 : 1.0;
+  auto cost = [&](int n) {
+    const int rest = mid_m * std::max(0, mid_n - 2 * n);
+    const double mids = rest == 0 ? 0.0 : rest % 512 == 0 ? rest / 512 * small : rest / 512 * small + (rest % 512 <= 256 ? half : small);
+    return (double)((nb_m * n + 255) / 256) * round + mids + (n > 0 && rest > 0 ? 0.2 : 0.0);
+  };
+  int best = 0;
+  double best_c = cost(0);
+  for (int n = nb_n; n > 0; --n)
+    if (cost(n) < best_c - 1e-9) best = n, best_c = cost(n);
+  return best;
+}
 
 struct Bump {
   char* base;
@@ -768,16 +788,16 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
         k.tiles_n = to - from;
         hipLaunchKernelGGL((stats_kernel<T, S>), dim3(pt_grid(((n + S::rows - 1) / S::rows) * (to - from))), dim3(64 * S::waves), 0, s, k);
       };
-      if (!big_tiles(n, a.V)) {
-        run(PtMid(), 0, (a.V + 127) / 128);
-      } else if (const int first = sample_tiles(n, a.V, a.top)) {
+      const int big = big_columns(n, a.V, a.dtype), mids = (a.V + 127) / 128;
+      if (const int first = sample_tiles(n, a.V, a.top)) {
         run(PtBig(), 0, first);
         hipLaunchKernelGGL(stats_threshold_kernel, dim3((n + 15) / 16), dim3(256), 16 * (size_t)(4 * first | 1) * 4, s, k.pmax, n, 4 * first,
                            a.top, thr);
         k.thr = thr;
         run(PtBig(), first, (a.V + 255) / 256);
       } else {
-        run(PtBig(), 0, (a.V + 255) / 256);
+        if (big) run(PtBig(), 0, big);
+        if (2 * big < mids) run(PtMid(), 2 * big, mids);
       }
     });
     FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, a.inv_t,
@@ -796,30 +816,45 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
   return ws.off;
 }
 
-// The slices of K of a product with few tiles: as many as make the rounds of 256 whole tiles (512 of the smaller) times a slice's length
-// shortest, each at least 512 long, with what the fp32 slabs cost to write and read again (5 TB/s against 1 PFLOP/s).
-static int out_slices(int M, int N, int K, int esz, int* k_slice) {
-  const bool big = big_tiles(M, N);
-  const int n0 = big ? tiles(M, N, 256, 256) : tiles(M, N, 128, 128), per = big ? 256 : 512, stage = 128 / esz;
-  const double flops = (big ? 2.0 * 65536 : 2.0 * 16384) * (esz == 4 ? 16 : 1) / 4e12 * (big ? 1 : 0.5);
-  int best = 1;
+// The slices of K of a product, and the row tiles of 256 that go first (see big_columns; the rest has none).  Few tiles over a long K
+// are cut along it: as many slices as make rounds times a slice's length shortest, each at least 512 long, with what the fp32
+// slabs cost to write and to read again (5 TB/s).
+struct OutPlan {
+  int slices, k_slice, big;
+};
+static OutPlan out_plan(int M, int N, int K, int dtype) {
+  const int stage = stage_of(dtype);
+  OutPlan best = {1, K, 0};
   double best_t = 1e30;
   for (int z = 1; z <= 64; ++z) {
-    const int q = ((K + z - 1) / z + stage - 1) / stage * stage;
+    const int q = whole((K + z - 1) / z, stage);
     if (z > 1 && (q < 512 || (K + q - 1) / q != z)) continue;
-    const double t = (double)((n0 * z + per - 1) / per) * q * flops + (z > 1 ? (double)z * M * N * 8 / 5e12 + 4e-6 : 0);
-    if (t < best_t) best_t = t, best = z;
+    const double us = dtype == kTokensF32 ? 8.0 : 1.0;  // of a stage, in big_columns' units
+    const double slabs = z > 1 ? z * ((double)M * N * 8 / 5e6) + 4 : 0;
+    for (int big = 0; big < 2; ++big) {
+      const int n = big ? tiles(M, N, 256, 256) * z : tiles(M, N, 128, 128) * z;
+      const double rounds = big ? std::ceil(n / 256.0) * (dtype == kTokensF32 ? 4.0 : 1.95)
+                                : n / 512 * (dtype == kTokensF32 ? 2.0 : 1.5) + (n % 512 == 0 ? 0.0 : n % 512 <= 256 ? 1.0 : dtype == kTokensF32 ? 2.0 : 1.5);
+      const double t = rounds * us * (q / stage + 3) + slabs;
+      if (t < best_t) best_t = t, best = {z, q, big ? (M + 255) / 256 : 0};
+    }
   }
-  *k_slice = ((K + best - 1) / best + stage - 1) / stage * stage;
+  if (best.slices == 1) best.big = big_columns(N, M, dtype);
   return best;
 }
 
 template <typename T, bool AK, bool WK>
-static void launch_out(OutArgs& o, hipStream_t s) {
-  if (big_tiles(o.M, o.N))
-    hipLaunchKernelGGL((out_kernel<T, AK, WK, PtBig>), dim3(pt_grid(tiles(o.M, o.N, 256, 256) * o.slices)), dim3(512), 0, s, o);
-  else
-    hipLaunchKernelGGL((out_kernel<T, AK, WK, PtMid>), dim3(pt_grid(tiles(o.M, o.N, 128, 128) * o.slices)), dim3(256), 0, s, o);
+static void launch_out(OutArgs& o, const OutPlan& p, hipStream_t s) {
+  auto run = [&](auto shape, int from, int to) {
+    using S = decltype(shape);
+    o.tile0 = from;
+    o.tiles_n = to - from;
+    const int n = (to - from) * ((o.N + S::cols - 1) / S::cols) * o.slices;
+    hipLaunchKernelGGL((out_kernel<T, AK, WK, S>), dim3(pt_grid(n)), dim3(64 * S::waves), 0, s, o);
+  };
+  const int mids = (o.M + 127) / 128;
+  if (p.big) run(PtBig(), 0, p.big);
+  if (2 * p.big < mids) run(PtMid(), 2 * p.big, mids);
   if (o.slices > 1) {
     const size_t n = (size_t)o.M * (o.lds / 4);
     hipLaunchKernelGGL(out_sum_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, o);
@@ -837,11 +872,10 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
   // sums over several chunks of rows are formed in fp32: in the output, or here
   const bool grads_f32 = a.grad_f32 || a.dtype == kTokensF32;
   float* const dw32 = chunks && !grads_f32 ? ws.take<float>((size_t)a.V * a.d) : nullptr;
-  int kh = 0, kw = 0;
   size_t slab = 0;
   for (int t0 = 0; t0 < a.T; t0 += rows) {
     const int n = std::min(rows, a.T - t0);
-    const int zh = out_slices(n, a.d, kv, esz, &kh), zw = out_slices(a.V, a.d, whole(n, stage), esz, &kw);
+    const int zh = out_plan(n, a.d, kv, a.dtype).slices, zw = out_plan(a.V, a.d, whole(n, stage), a.dtype).slices;
     slab = std::max(slab, std::max(zh > 1 ? (size_t)zh * n * lds : 0, zw > 1 ? (size_t)zw * a.V * lds : 0));
   }
   float* const slabs = ws.take<float>(slab);
@@ -852,8 +886,8 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
   for (int t0 = 0; t0 < a.T; t0 += rows) {
     const int n = std::min(rows, a.T - t0);
     const void* const hp = (const char*)h.p + (size_t)t0 * h.ld * esz;
-    const DzArgs k = {hp, w.p, h.ld, w.ld, n, a.V, whole(a.d, stage), a.targets + t0, a.lse + t0, (a.d_entropy ? a.entropy : a.lse) + t0, a.d_logprob + t0,
-                      a.d_entropy ? a.d_entropy + t0 : nullptr, scaled ? scale : nullptr, a.inv_t, dz, ldz, whole(n, stage)};
+    DzArgs k = {hp, w.p, h.ld, w.ld, n, a.V, whole(a.d, stage), a.targets + t0, a.lse + t0, (a.d_entropy ? a.entropy : a.lse) + t0, a.d_logprob + t0,
+                      a.d_entropy ? a.d_entropy + t0 : nullptr, scaled ? scale : nullptr, a.inv_t, dz, ldz, whole(n, stage), 0, 0};
     OutArgs oh = {}, ow = {};
     oh.A = dz;
     oh.lda = ldz;
@@ -862,7 +896,9 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
     oh.M = n;
     oh.N = a.d;
     oh.K = kv;
-    oh.slices = out_slices(n, a.d, kv, esz, &oh.k_slice);
+    const OutPlan ph = out_plan(n, a.d, kv, a.dtype);
+    oh.slices = ph.slices;
+    oh.k_slice = ph.k_slice;
     oh.out = (char*)a.d_hidden + (size_t)t0 * a.d * (grads_f32 ? 4 : 2);
     oh.ldo = a.d;
     oh.f32 = grads_f32;
@@ -873,7 +909,9 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
     ow.M = a.V;
     ow.N = a.d;
     ow.K = whole(n, stage);
-    ow.slices = out_slices(a.V, a.d, ow.K, esz, &ow.k_slice);
+    const OutPlan pw = out_plan(a.V, a.d, ow.K, a.dtype);
+    ow.slices = pw.slices;
+    ow.k_slice = pw.k_slice;
     ow.out = dw32 ? (void*)dw32 : a.d_weight;
     ow.ldo = a.d;
     ow.f32 = grads_f32 || dw32;
@@ -883,12 +921,17 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
     oh.lds = ow.lds = lds;
     by_type(a.dtype, [&](auto t) {
       using T = decltype(t);
-      if (big_tiles(n, a.V))
-        hipLaunchKernelGGL((dz_kernel<T, PtBig>), dim3(pt_grid(tiles(n, a.V, 256, 256))), dim3(512), 0, s, k);
-      else
-        hipLaunchKernelGGL((dz_kernel<T, PtMid>), dim3(pt_grid(tiles(n, a.V, 128, 128))), dim3(256), 0, s, k);
-      launch_out<T, false, true>(oh, s);
-      launch_out<T, true, true>(ow, s);
+      auto run = [&](auto shape, int from, int to) {
+        using S = decltype(shape);
+        k.tile0 = from;
+        k.tiles_n = to - from;
+        hipLaunchKernelGGL((dz_kernel<T, S>), dim3(pt_grid(((n + S::rows - 1) / S::rows) * (to - from))), dim3(64 * S::waves), 0, s, k);
+      };
+      const int big = big_columns(n, a.V, a.dtype), mids = (a.V + 127) / 128;
+      if (big) run(PtBig(), 0, big);
+      if (2 * big < mids) run(PtMid(), 2 * big, mids);
+      launch_out<T, false, true>(oh, ph, s);
+      launch_out<T, true, true>(ow, pw, s);
     });
     if ((*err = hipGetLastError()) != hipSuccess) return ws.off;
   }
