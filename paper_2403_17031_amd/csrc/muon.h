@@ -23,7 +23,7 @@ struct MuonScalars {
   float decay;                  // param = decay param - lr rms sqrt(max(rows, cols)) O
   double lr_rms;
 };
-constexpr int kMuonGroup = 24;  // most matrices of a call
+constexpr int kMuonGroup = 48;  // most matrices of a call
 // Workspace bytes of a call on matrices of these sizes.
 size_t muon_workspace_bytes(const MuonMatrix* ms, int count);
 hipError_t launch_muon(const MuonMatrix* ms, int count, const MuonScalars& c, void* workspace, hipStream_t s);

@@ -16,6 +16,8 @@
 // with zeros to multiples of 64, which the iteration keeps zero.  All matrices of a call share its launches.
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
+#include <cstring>
 
 #include "common.h"
 #include "muon.h"
@@ -27,10 +29,26 @@ namespace {
 
 using PtBig = PtShape<2, 4, 4, 2>;
 using PtMid = PtShape<2, 2, 2, 2>;
+using PtSmall = PtShape<2, 1, 1, 2, 4>;  // 64 x 64, two waves, a ring of four stages
+
+template <typename S>
+__device__ __forceinline__ char* muon_wave_lds(char* ring, char* la0, char* lw0, char* la1, char* lw1) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if constexpr (S::RING > 2) return ring + wave * 16384;
+  else return pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
+}
+// One tile's product, whichever way the shape keeps its stages, and the LDS a wave has afterwards.
+#define MUON_LDS(S) __shared__ __attribute__((aligned(16))) char lds[S::RING > 2 ? S::RING * S::stage : 16];          \
+  __shared__ __attribute__((aligned(16))) char la0[S::RING > 2 ? 16 : S::rows * 128], lw0[S::RING > 2 ? 16 : S::cols * 128]; \
+  __shared__ __attribute__((aligned(16))) char la1[S::RING > 2 ? 16 : S::rows * 128], lw1[S::RING > 2 ? 16 : S::cols * 128];
+#define MUON_WAVE_LDS muon_wave_lds<S>(lds, la0, lw0, la1, lw1)
+#define MUON_PRODUCT(AK, WK, ...)                                                               \
+  if constexpr (S::RING > 2) pt_product_ring<half_t, AK, WK, S>(__VA_ARGS__, lds, acc);         \
+  else pt_product<half_t, AK, WK, S>(__VA_ARGS__, la0, lw0, la1, lw1, acc)
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kXScale = 2048.f, kAScale = 4096.f;
-constexpr int kProbs = kMuonGroup;
+constexpr int kProbs = kMuonGroup;  // of a launch
 constexpr int kNormElems = 16384;  // elements of a block of the norm
 constexpr size_t kGroupElems = (size_t)1 << 28;
 
@@ -44,29 +62,50 @@ struct Prob {
   float step;             // lr rms sqrt(max(rows, cols))
   int vec;                // 16-byte accesses to the caller's arrays: eight elements of a row start where they may
 };
+enum Part { kNorm, kSplit, kGram, kPoly, kUpdate, kParts };
+// What the launches of a group share.  It lies in the workspace, put there before them: as an argument of each, it would be fetched
+// from the argument segment, line after line, by every block.
 struct Group {
-  Prob p[kProbs];
-  uint32_t first[kProbs];  // first work item of each
-  int count;
-  uint32_t items;
   MuonScalars c;
+  int count;
+  uint32_t items[kParts];         // all work items
+  uint32_t first[kParts][kProbs]; // first work item of each problem, ~0 beyond the last
+  uint32_t start[kParts][9];      // tiles that are dealt in runs: where each XCD's begins; split[]: every problem is dealt to all XCDs
+  uint32_t split[kParts];         // (items are then eighths of them)
+  Prob p[kProbs];
 };
+static_assert(kProbs < 64, "a problem is found by the lanes of a wave");
 
-// The problem of a work item, and the item's index within it.
-__device__ __forceinline__ const Prob& find_prob(const Group& g, uint32_t item, int& index) {
-  int at = 0;
-  for (int i = 1; i < g.count; ++i)
-    if (g.first[i] <= item) at = i;
-  index = (int)(item - g.first[at]);
-  return g.p[at];
+struct Words {
+  uint32_t w[960];
+};
+__global__ void __launch_bounds__(256) muon_table_kernel(Words in, int n, uint32_t* out) {
+  for (int i = threadIdx.x; i < n; i += 256) out[i] = in.w[i];
 }
-// Tiles: block b runs on XCD b % 8 and every XCD takes an eighth of each problem's tiles, a contiguous run, so that the XCDs
-// have the same work whatever the problems' sizes (first[] then counts eighths).  -1: none.
-__device__ __forceinline__ int find_tile(const Group& g, const Prob*& p) {
-  int index;
-  p = &find_prob(g, blockIdx.x >> 3, index);
-  const int at = (int)(p - g.p), eighth = (int)((at + 1 < g.count ? g.first[at + 1] : g.items) - g.first[at]);
-  return (int)(blockIdx.x & 7) * eighth + index;
+
+// The problem of a work item of `part`, the item's index within it, and how many it has.
+__device__ __forceinline__ const Prob& find_prob(const Group* __restrict__ g, Part part, uint32_t item, int& index, int& of) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t first = lane < kProbs ? g->first[part][lane] : ~0u;
+  const int at = __builtin_amdgcn_readfirstlane(__popcll(__ballot(first <= item)) - 1);  // (first[0] is 0)
+  const uint32_t from = (uint32_t)__builtin_amdgcn_readlane((int)first, at), to = (uint32_t)__builtin_amdgcn_readlane((int)first, at + 1);
+  index = (int)(item - from);
+  of = (int)(min(to, g->items[part]) - from);
+  return g->p[at];
+}
+// Tiles: block b runs on XCD b % 8.  Few problems of many tiles: every XCD takes an eighth of each, a run of neighbours, and all work
+// on a problem at a time, whose operands then are in the last cache.  Many of few tiles: an XCD takes a run of neighbouring tiles of as
+// much work as the others', so that a problem's operands go to one XCD or two (24 matrices of width 512: A^2 21 -> 13 us a launch;
+// eight of the 2.8B layers the other way round 5 % slower).  -1: none.
+__device__ __forceinline__ const Prob& find_tile(const Group* __restrict__ g, Part part, int& tile) {
+  const uint32_t x = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  const bool split = g->split[part] != 0;
+  const uint32_t item = split ? slot : g->start[part][x] + slot;
+  const bool none = !split && item >= g->start[part][x + 1];
+  int index, of;
+  const Prob& p = find_prob(g, part, min(item, g->items[part] - 1), index, of);
+  tile = __builtin_amdgcn_readfirstlane(none ? -1 : split ? (int)x * of + index : index);
+  return p;
 }
 
 __device__ __forceinline__ float bf16_at(const void* p, size_t i) { return __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16); }
@@ -126,10 +165,11 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 }
 
 // The momentum's update, and the sum of squares of 16,384 elements.
-__global__ void __launch_bounds__(256) muon_norm_kernel(Group g) {
+__global__ void __launch_bounds__(256) muon_norm_kernel(const Group* __restrict__ g) {
+  const MuonScalars c = g->c;
   __shared__ double sh[4];
-  int block;
-  const Prob& p = find_prob(g, blockIdx.x, block);
+  int block, of;
+  const Prob& p = find_prob(g, kNorm, blockIdx.x, block, of);
   const size_t n = (size_t)p.m.rows * p.m.cols, i0 = (size_t)block * kNormElems, i1 = min(n, i0 + kNormElems);
   double sum = 0.0;
   if (p.vec) {  // (i1 - i0 is a multiple of eight)
@@ -142,21 +182,21 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(Group g) {
           const pt_f32x4 gr = *(const pt_f32x4*)(p.m.grad + i + 4 * k);
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            m[u] = g.c.beta * m[u] + g.c.omb * (g.c.grad_scale * gr[u]);
-            v[4 * k + u] = g.c.nesterov ? g.c.omb * (g.c.grad_scale * gr[u]) + g.c.beta * m[u] : m[u];
+            m[u] = c.beta * m[u] + c.omb * (c.grad_scale * gr[u]);
+            v[4 * k + u] = c.nesterov ? c.omb * (c.grad_scale * gr[u]) + c.beta * m[u] : m[u];
           }
           *(pt_f32x4*)(p.m.moment + i + 4 * k) = m;
         }
       } else {
-        source8(p, g.c, i, v);
+        source8(p, c, i, v);
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) sum += (double)v[u] * (double)v[u];
     }
   }
   for (size_t i = p.vec ? i1 : i0 + threadIdx.x; i < i1; i += 256) {
-    if (!p.m.src) p.m.moment[i] = g.c.beta * p.m.moment[i] + g.c.omb * (g.c.grad_scale * p.m.grad[i]);
-    const double v = source_at(p, g.c, i);
+    if (!p.m.src) p.m.moment[i] = c.beta * p.m.moment[i] + c.omb * (c.grad_scale * p.m.grad[i]);
+    const double v = source_at(p, c, i);
     sum += v * v;
   }
   sum = wave_sum_f64(sum);
@@ -165,9 +205,10 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(Group g) {
   if (threadIdx.x == 0) p.part[block] = (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
-__global__ void __launch_bounds__(256) muon_scale_kernel(Group g) {
+__global__ void __launch_bounds__(256) muon_scale_kernel(const Group* __restrict__ g) {
+  const MuonScalars c = g->c;
   __shared__ double sh[256];
-  const Prob& p = g.p[blockIdx.x];
+  const Prob& p = g->p[blockIdx.x];
   const int blocks = (int)(((size_t)p.m.rows * p.m.cols + kNormElems - 1) / kNormElems);
   double sum = 0.0;
   for (int i = threadIdx.x; i < blocks; i += 256) sum += p.part[i];
@@ -177,13 +218,14 @@ __global__ void __launch_bounds__(256) muon_scale_kernel(Group g) {
     if ((int)threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
     __syncthreads();
   }
-  if (threadIdx.x == 0) *p.scale = (float)((double)kXScale / (sqrt(sh[0]) + (double)g.c.eps));
+  if (threadIdx.x == 0) *p.scale = (float)((double)kXScale / (sqrt(sh[0]) + (double)c.eps));
 }
 
 // X = scale * source as two halves, zero in the padding; eight columns a thread.
-__global__ void __launch_bounds__(256) muon_split_kernel(Group g) {
-  int block;
-  const Prob& p = find_prob(g, blockIdx.x, block);
+__global__ void __launch_bounds__(256) muon_split_kernel(const Group* __restrict__ g) {
+  const MuonScalars c = g->c;
+  int block, of;
+  const Prob& p = find_prob(g, kSplit, blockIdx.x, block, of);
   const uint32_t chunk = (uint32_t)block * 256 + threadIdx.x, per_row = (uint32_t)p.ld / 8;
   const uint32_t row = chunk / per_row, col = (chunk - row * per_row) * 8;
   if (row >= (uint32_t)p.rp) return;
@@ -193,10 +235,10 @@ __global__ void __launch_bounds__(256) muon_split_kernel(Group g) {
   float v[8];
   const size_t at = (size_t)row * p.m.cols + col;
   if (p.vec && row < (uint32_t)p.m.rows && col + 8 <= (uint32_t)p.m.cols) {
-    source8(p, g.c, at, v);
+    source8(p, c, at, v);
   } else {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = row < (uint32_t)p.m.rows && col + u < (uint32_t)p.m.cols ? source_at(p, g.c, at + u) : 0.f;
+    for (int u = 0; u < 8; ++u) v[u] = row < (uint32_t)p.m.rows && col + u < (uint32_t)p.m.cols ? source_at(p, c, at + u) : 0.f;
   }
 #pragma unroll
   for (int u = 0; u < 8; ++u) {
@@ -243,66 +285,64 @@ __device__ __forceinline__ void store_symmetric(pt_f32x16 (&acc)[S::NT][S::MT], 
     pt_hand_out_transposed<MT>(ep, lane, acc, [&](int c, int r, pt_u32x4 v) {
       if (row0 + r < ld) *(pt_u32x4*)(out + (size_t)(col0 + c) * ld + row0 + r) = v;
     });
-  pt_hand_out<8, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, const float(&v)[8], int) {
+  pt_hand_out<8, MT, (MT > 1 ? 64 : 32)>(ep, lane, acc, PtNothing(), [&](int r, int c, const float(&v)[8], int) {
     if (row0 + r < ld) *(pt_u32x4*)(out + (size_t)(row0 + r) * ld + col0 + c) = pt_pack8<half_t>(v);
   });
 }
 
 // A = X X^T (the shorter side's), scaled
 template <typename S>
-__global__ void __launch_bounds__(64 * S::waves, 2) muon_gram_kernel(Group g, int cur) {
-  PT_SHARED(S)
-  const Prob* pp;
-  const int tile = find_tile(g, pp);
-  const Prob& p = *pp;
+__global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_gram_kernel(const Group* __restrict__ g, int cur) {
+  MUON_LDS(S)
+  int tile;
+  const Prob& p = find_tile(g, kGram, tile);
+  if (tile < 0) return;
   int tm, tn;
   pt_tile_triangle(tile, tm, tn);
   if (tm * S::rows >= p.sp) return;
   pt_f32x16 acc[S::NT][S::MT];
   const half_t* const x = p.xh[cur];
   if (p.m.rows > p.m.cols)
-    pt_product<half_t, true, true, S>(x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp, la0, lw0, la1, lw1, acc);
+    MUON_PRODUCT(true, true, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp);
   else
-    pt_product<half_t, false, false, S>(x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld, la0, lw0, la1, lw1, acc);
+    MUON_PRODUCT(false, false, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld);
   store_symmetric<S, false>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f,
-                     pt_wave_lds<S>(la0, lw0, la1, lw1, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)));
+                     MUON_WAVE_LDS);
 }
 
 // B = b A + c A^2
 template <typename S>
-__global__ void __launch_bounds__(64 * S::waves, 2) muon_poly_kernel(Group g) {
-  PT_SHARED(S)
-  const Prob* pp;
-  const int tile = find_tile(g, pp);
-  const Prob& p = *pp;
+__global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_poly_kernel(const Group* __restrict__ g) {
+  MUON_LDS(S)
+  int tile;
+  const Prob& p = find_tile(g, kPoly, tile);
+  if (tile < 0) return;
   int tm, tn;
   pt_tile_triangle(tile, tm, tn);
   if (tm * S::rows >= p.sp) return;
   pt_f32x16 acc[S::NT][S::MT];
-  pt_product<half_t, false, false, S>(p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp, la0, lw0, la1, lw1, acc);
+  MUON_PRODUCT(false, false, p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp);
   store_symmetric<S, true>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB,
-                     pt_wave_lds<S>(la0, lw0, la1, lw1, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)));
+                     MUON_WAVE_LDS);
 }
 
 // X <- a X + B X, or after the last step what becomes of it
 template <typename S>
-__global__ void __launch_bounds__(64 * S::waves, 2) muon_update_kernel(Group g, int cur, int last) {
-  PT_SHARED(S)
+__global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_update_kernel(const Group* __restrict__ g, int cur, int last) {
+  const MuonScalars c = g->c;
+  MUON_LDS(S)
   constexpr int MT = S::MT;
-  const Prob* pp;
-  const int tile = find_tile(g, pp);
-  const Prob& p = *pp;
+  int tile;
+  const Prob& p = find_tile(g, kUpdate, tile);
   const int nb_m = (p.rp + S::rows - 1) / S::rows, nb_n = (p.ld + S::cols - 1) / S::cols;
-  if (tile >= nb_m * nb_n) return;
+  if (tile < 0 || tile >= nb_m * nb_n) return;
   int tm, tn;
   pt_tile_pos(tile, nb_m, nb_n, tm, tn);
   pt_f32x16 acc[2][MT];
   if (p.m.rows > p.m.cols)
-    pt_product<half_t, false, false, S>(p.xh[cur], p.ld, tm * S::rows, p.rp, p.b, p.sp, tn * S::cols, p.sp, 0, p.sp, la0, lw0, la1,
-                                        lw1, acc);
+    MUON_PRODUCT(false, false, p.xh[cur], p.ld, tm * S::rows, p.rp, p.b, p.sp, tn * S::cols, p.sp, 0, p.sp);
   else
-    pt_product<half_t, false, true, S>(p.b, p.sp, tm * S::rows, p.sp, p.xh[cur], p.ld, tn * S::cols, p.ld, 0, p.sp, la0, lw0, la1,
-                                       lw1, acc);
+    MUON_PRODUCT(false, true, p.b, p.sp, tm * S::rows, p.sp, p.xh[cur], p.ld, tn * S::cols, p.ld, 0, p.sp);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -314,19 +354,20 @@ __global__ void __launch_bounds__(64 * S::waves, 2) muon_update_kernel(Group g, 
   const half_t* const xl = p.xl[cur] + (size_t)row0 * p.ld + col0;
   half_t* const nh = p.xh[cur ^ 1] + (size_t)row0 * p.ld + col0;
   half_t* const nl = p.xl[cur ^ 1] + (size_t)row0 * p.ld + col0;
-  f16x8 h[8], l[8];  // this pass's X, requested before the results go through LDS
-  pt_hand_out<8, MT>(
-      pt_wave_lds<S>(la0, lw0, la1, lw1, wave), lane, acc,
+  f16x8 h[MT > 1 ? 8 : 4], l[MT > 1 ? 8 : 4];  // this pass's X, requested before the results go through LDS
+  constexpr int PR = MT > 1 ? 64 : 32, NI = PR / 8;
+  pt_hand_out<8, MT, PR>(
+      MUON_WAVE_LDS, lane, acc,
       [&](int pass) {
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-          const size_t i = (size_t)min(64 * pass + 8 * it + rd_row, p.rp - 1 - row0) * p.ld + 8 * rd_c;
+        for (int it = 0; it < NI; ++it) {
+          const size_t i = (size_t)min(PR * pass + 8 * it + rd_row, p.rp - 1 - row0) * p.ld + 8 * rd_c;
           h[it] = *(const f16x8*)(xh + i);
           l[it] = *(const f16x8*)(xl + i);
         }
       },
-      [&](int r, int c, float(&v)[8], int it) {
-        const int row = row0 + r, col = col0 + c;
+      [&](int r, int cc, float(&v)[8], int it) {
+        const int row = row0 + r, col = col0 + cc;
         if (row >= p.rp) return;
 #pragma unroll
         for (int u = 0; u < 8; ++u) v[u] = fmaf(v[u], 1.f / kAScale, kA * ((float)h[it][u] + (float)l[it][u]));
@@ -339,7 +380,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) muon_update_kernel(Group g, 
             a[u] = hu;
             b[u] = lu;
           }
-          const size_t i = (size_t)r * p.ld + c;
+          const size_t i = (size_t)r * p.ld + cc;
           *(f16x8*)(nh + i) = a;
           *(f16x8*)(nl + i) = b;
           return;
@@ -354,7 +395,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) muon_update_kernel(Group g, 
             for (int k = 0; k < 2; ++k) {
               pt_f32x4 w = *(const pt_f32x4*)(p.m.param + o + 4 * k);
 #pragma unroll
-              for (int u = 0; u < 4; ++u) v[4 * k + u] = w[u] = g.c.decay * w[u] - p.step * v[4 * k + u];
+              for (int u = 0; u < 4; ++u) v[4 * k + u] = w[u] = c.decay * w[u] - p.step * v[4 * k + u];
               *(pt_f32x4*)(p.m.param + o + 4 * k) = w;
             }
           }
@@ -368,7 +409,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) muon_update_kernel(Group g, 
           if (p.m.src) {
             p.m.out[o + u] = pt_bits(bfloat(), v[u]);
           } else {
-            const float w = g.c.decay * p.m.param[o + u] - p.step * v[u];
+            const float w = c.decay * p.m.param[o + u] - p.step * v[u];
             p.m.param[o + u] = w;
             if (p.m.param_bf16) p.m.param_bf16[o + u] = pt_bits(bfloat(), w);
           }
@@ -393,7 +434,7 @@ int group_end(const MuonMatrix* ms, int from, int count) {
 
 // Lays the group's buffers into the workspace from `base` on (null: measures); returns the end.
 size_t lay_out(Group* g, char* base, const MuonMatrix* ms, int from, int to) {
-  size_t off = 0;
+  size_t off = align256(sizeof(Group));  // (the table's place)
   auto take = [&](size_t bytes) {
     char* const at = base ? base + off : nullptr;
     off += align256(bytes);
@@ -419,12 +460,13 @@ size_t lay_out(Group* g, char* base, const MuonMatrix* ms, int from, int to) {
 }
 
 template <typename F>
-void number(Group& g, F items) {
-  g.items = 0;
-  for (int i = 0; i < g.count; ++i) {
-    g.first[i] = g.items;
-    g.items += (uint32_t)items(g.p[i]);
+void number(Group& g, Part part, F items) {
+  uint32_t n = 0;
+  for (int i = 0; i < kProbs; ++i) {
+    g.first[part][i] = i < g.count ? n : ~0u;
+    if (i < g.count) n += (uint32_t)items(g.p[i]);
   }
+  g.items[part] = n;
 }
 int up(int n, int t) { return (n + t - 1) / t; }
 int triangle(int n) { return n * (n + 1) / 2; }
@@ -434,9 +476,9 @@ struct Tiles {
   int (*count)(const Prob&, int tile);
   int (*depth)(const Prob&);
 };
-const Tiles kGram = {[](const Prob& p, int t) { return triangle(up(p.sp, t)); }, [](const Prob& p) { return std::max(p.rp, p.ld); }};
-const Tiles kPoly = {[](const Prob& p, int t) { return triangle(up(p.sp, t)); }, [](const Prob& p) { return p.sp; }};
-const Tiles kUpdate = {[](const Prob& p, int t) { return up(p.rp, t) * up(p.ld, t); }, [](const Prob& p) { return p.sp; }};
+const Tiles kGramTiles = {[](const Prob& p, int t) { return triangle(up(p.sp, t)); }, [](const Prob& p) { return std::max(p.rp, p.ld); }};
+const Tiles kPolyTiles = {[](const Prob& p, int t) { return triangle(up(p.sp, t)); }, [](const Prob& p) { return p.sp; }};
+const Tiles kUpdateTiles = {[](const Prob& p, int t) { return up(p.rp, t) * up(p.ld, t); }, [](const Prob& p) { return p.sp; }};
 
 // Rounds that the tiles take on `slots` places, in units of the deepest tile's time.
 double rounds(const Group& g, const Tiles& t, int tile, int slots) {
@@ -451,12 +493,40 @@ double rounds(const Group& g, const Tiles& t, int tile, int slots) {
 // stage).
 bool takes_big(const Group& g, const Tiles& t) { return 1.3 * rounds(g, t, 256, 256) <= rounds(g, t, 128, 512); }
 
+enum Shape { kBig, kMid, kSmall };
+constexpr int kTile[] = {256, 128, 64}, kThreads[] = {512, 256, 128};
+
+#include <cstdlib>
+Shape number_tiles(Group& g, Part part, const Tiles& t) {
+  static const char* e = getenv("MUON_SHAPE");
+  const Shape c = e ? (Shape)(e[part - kGram] - '0') : takes_big(g, t) ? kBig : kMid;
+  double work = 0;
+  int tiles = 0;
+  for (int i = 0; i < g.count; ++i) {
+    work += (double)t.count(g.p[i], kTile[c]) * t.depth(g.p[i]);
+    tiles += t.count(g.p[i], kTile[c]);
+  }
+  g.split[part] = tiles >= 32 * g.count;
+  if (g.split[part]) {
+    number(g, part, [&](const Prob& p) { return up(t.count(p, kTile[c]), 8); });
+    return c;
+  }
+  number(g, part, [&](const Prob& p) { return t.count(p, kTile[c]); });
+  double done = 0;
+  int x = 0;
+  for (int i = 0; i < g.count; ++i) {
+    const double each = t.depth(g.p[i]), end = done + each * t.count(g.p[i], kTile[c]);
+    for (; x < 8 && work * x / 8 < end; ++x) g.start[part][x] = g.first[part][i] + (uint32_t)((work * x / 8 - done) / each);
+    done = end;
+  }
+  for (; x < 9; ++x) g.start[part][x] = g.items[part];
+  return c;
+}
 template <typename K, typename... A>
-void on_tiles(Group& g, const Tiles& t, hipStream_t s, K big, K mid, A... args) {
-  const bool b = takes_big(g, t);
-  number(g, [&](const Prob& p) { return up(t.count(p, b ? 256 : 128), 8); });
-  if (b) hipLaunchKernelGGL(big, dim3(8 * g.items), dim3(64 * PtBig::waves), 0, s, g, args...);
-  else hipLaunchKernelGGL(mid, dim3(8 * g.items), dim3(64 * PtMid::waves), 0, s, g, args...);
+void on_tiles(const Group& g, const Group* dev, Part part, Shape c, hipStream_t s, K big, K mid, K small, A... args) {
+  uint32_t most = g.split[part] ? g.items[part] : 0;
+  for (int x = 0; x < 8 && !g.split[part]; ++x) most = std::max(most, g.start[part][x + 1] - g.start[part][x]);
+  hipLaunchKernelGGL(c == kBig ? big : c == kMid ? mid : small, dim3(8 * most), dim3(kThreads[c]), 0, s, dev, args...);
 }
 
 }  // namespace
@@ -486,16 +556,26 @@ hipError_t launch_muon(const MuonMatrix* ms, int count, const MuonScalars& c, vo
       g.p[i].vec = m.cols % 8 == 0 && (bases & 15) == 0;
     }
     std::sort(g.p, g.p + g.count, [](const Prob& a, const Prob& b) { return std::max(a.rp, a.ld) > std::max(b.rp, b.ld); });
-    number(g, [](const Prob& p) { return norm_blocks(p.m.rows, p.m.cols); });
-    hipLaunchKernelGGL(muon_norm_kernel, dim3(g.items), dim3(256), 0, s, g);
-    hipLaunchKernelGGL(muon_scale_kernel, dim3(g.count), dim3(256), 0, s, g);
-    number(g, [](const Prob& p) { return (int)(((size_t)p.rp * p.ld / 8 + 255) / 256); });
-    hipLaunchKernelGGL(muon_split_kernel, dim3(g.items), dim3(256), 0, s, g);
+    number(g, kNorm, [](const Prob& p) { return norm_blocks(p.m.rows, p.m.cols); });
+    number(g, kSplit, [](const Prob& p) { return (int)(((size_t)p.rp * p.ld / 8 + 255) / 256); });
+    const Shape gram = number_tiles(g, kGram, kGramTiles), poly = number_tiles(g, kPoly, kPolyTiles), update = number_tiles(g, kUpdate, kUpdateTiles);
+    Group* const dev = (Group*)workspace;
+    const size_t words = (offsetof(Group, p) + g.count * sizeof(Prob)) / 4;
+    for (size_t at = 0; at < words; at += sizeof(Words) / 4) {
+      const int n = (int)std::min(words - at, sizeof(Words) / 4);
+      Words w;
+      std::memcpy(w.w, (const uint32_t*)&g + at, (size_t)n * 4);
+      hipLaunchKernelGGL(muon_table_kernel, dim3(1), dim3(256), 0, s, w, n, (uint32_t*)dev + at);
+    }
+    hipLaunchKernelGGL(muon_norm_kernel, dim3(g.items[kNorm]), dim3(256), 0, s, dev);
+    hipLaunchKernelGGL(muon_scale_kernel, dim3(g.count), dim3(256), 0, s, dev);
+    hipLaunchKernelGGL(muon_split_kernel, dim3(g.items[kSplit]), dim3(256), 0, s, dev);
     for (int k = 0; k < c.steps; ++k) {
       const int cur = k & 1;
-      on_tiles(g, kGram, s, muon_gram_kernel<PtBig>, muon_gram_kernel<PtMid>, cur);
-      on_tiles(g, kPoly, s, muon_poly_kernel<PtBig>, muon_poly_kernel<PtMid>);
-      on_tiles(g, kUpdate, s, muon_update_kernel<PtBig>, muon_update_kernel<PtMid>, cur, (int)(k + 1 == c.steps));
+      on_tiles(g, dev, kGram, gram, s, muon_gram_kernel<PtBig>, muon_gram_kernel<PtMid>, muon_gram_kernel<PtSmall>, cur);
+      on_tiles(g, dev, kPoly, poly, s, muon_poly_kernel<PtBig>, muon_poly_kernel<PtMid>, muon_poly_kernel<PtSmall>);
+      on_tiles(g, dev, kUpdate, update, s, muon_update_kernel<PtBig>, muon_update_kernel<PtMid>, muon_update_kernel<PtSmall>, cur,
+               (int)(k + 1 == c.steps));
     }
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     from = to;

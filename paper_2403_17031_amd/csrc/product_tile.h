@@ -44,11 +44,11 @@ __device__ __forceinline__ pt_f32x16 pt_mma(float, pt_u32x4 w, pt_u32x4 a, pt_f3
 #define PT_GLOBAL(p) ((const __attribute__((address_space(1))) void*)(p))
 #define PT_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
-// WM x WN waves of MT x NT accumulators of 32 x 32
-template <int WM_, int WN_, int MT_, int NT_>
+// WM x WN waves of MT x NT accumulators of 32 x 32; RING stages of LDS (2: see pt_product, more: pt_product_ring)
+template <int WM_, int WN_, int MT_, int NT_, int RING_ = 2>
 struct PtShape {
-  static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_;
-  static constexpr int waves = WM * WN, rows = 32 * MT * WM, cols = 32 * NT * WN;
+  static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, RING = RING_;
+  static constexpr int waves = WM * WN, rows = 32 * MT * WM, cols = 32 * NT * WN, stage = (rows + cols) * 128;
 };
 
 // One operand's tile loads: this lane's 16-byte chunks of a stage, as byte offsets from a uniform base.
@@ -64,6 +64,10 @@ struct PtLoads {
   __device__ static int chunk(int i, int wave, int lane) {
     const int r = lds_row(i, wave, lane), pos = ((1024 * (L * wave + i) + 16 * lane) % RB) / 16;
     return KM ? pos ^ (2 * (r & 3)) : pos ^ ((r >> 1) & 7);
+  }
+  // the same through load_to_lds, for a caller that counts its waits
+  __device__ __forceinline__ void load_counted(uint32_t lds, int stage, int i, int wave) const {
+    load_to_lds(base + stage * step, off[i], lds + 1024 * (L * wave + i));
   }
   // the operand from its row r0 (of `extent`) on, from k0 on
   __device__ void init(const void* p, uint32_t ld, int r0, int extent, int k0, int wave, int lane) {
@@ -219,6 +223,99 @@ __device__ __forceinline__ void pt_product(const void* A, uint32_t lda, int m0, 
   if (kt < nk) stage(kt, la0, lw0, la1, lw1);
 }
 
+// The same with a ring of S::RING stages, all but one of them under way while one is used: for launches whose tiles do not fill
+// the chip, where a stage's loads take longer than its multiplications.  The compiler does not know of the loads; what orders
+// them is the counted wait before the barrier.  Ends as pt_product does.
+template <typename T, bool AK, bool WK, typename S>
+__device__ __forceinline__ void pt_product_ring(const void* A, uint32_t lda, int m0, int M, const void* W, uint32_t ldw, int n0, int N,
+                                                int k0, int k1, char* lds, pt_f32x16 (&acc)[S::NT][S::MT]) {
+  constexpr int MT = S::MT, NT = S::NT, F = MT + NT, D = S::RING;
+  using LA = PtLoads<T, AK, S::rows, S::waves>;
+  using LW = PtLoads<T, WK, S::cols, S::waves>;
+  constexpr int NL = LA::L + LW::L;
+  static_assert((D - 1) * NL < 64, "the wait counts to 63");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / S::WN) * 32 * MT, wn = (wave % S::WN) * 32 * NT;
+  LA ga;
+  LW gw;
+  ga.init(A, lda, m0, M, k0, wave, lane);
+  gw.init(W, ldw, n0, N, k0, wave, lane);
+  PtFrags<T, AK, S::rows> ra[MT];
+  PtFrags<T, WK, S::cols> rw[NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) ra[i].init(wm + 32 * i, lane);
+#pragma unroll
+  for (int j = 0; j < NT; ++j) rw[j].init(wn + 32 * j, lane);
+  const int nk = (k1 - k0) / LA::KD;
+  const uint32_t lds_at = (uint32_t)(uintptr_t)PT_LDS(lds);
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.f;
+  auto load_all = [&](int slot, int stage) {
+    const uint32_t at = lds_at + slot * S::stage;
+#pragma unroll
+    for (int n = 0; n < LA::L; ++n) ga.load_counted(at, stage, n, wave);
+#pragma unroll
+    for (int n = 0; n < LW::L; ++n) gw.load_counted(at + S::rows * 128, stage, n, wave);
+  };
+  // until at most `left` stages of this wave's loads are under way, its fragments read, and every wave here
+  auto wait = [&](int left) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    auto upto = [&](auto n) {
+      constexpr int v = decltype(n)::value * NL;
+      __builtin_amdgcn_s_waitcnt(0x0070 | (v & 15) | ((v >> 4) << 14));
+    };
+    if (D > 3 && left >= 3) upto(std::integral_constant<int, (D > 3 ? 3 : 0)>{});
+    else if (D > 2 && left == 2) upto(std::integral_constant<int, 2>{});
+    else if (left == 1) upto(std::integral_constant<int, 1>{});
+    else upto(std::integral_constant<int, 0>{});
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  pt_u32x4 fa[2][MT], fw[2][NT];
+  auto frags = [&](int slot, int s, int buf) {
+    const char* const la = lds + slot * S::stage;
+#pragma unroll
+    for (int n = 0; n < MT; ++n) fa[buf][n] = ra[n].read(la, s, lane);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) fw[buf][n] = rw[n].read(la + S::rows * 128, s, lane);
+  };
+  auto mul = [&](int buf) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[j][i] = pt_mma(T(), fw[buf][j], fa[buf][i], acc[j][i]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll
+  for (int u = 0; u < D - 1; ++u)
+    if (u < nk) load_all(u, u);
+  wait(min(D - 2, nk - 1));
+  frags(0, 0, 0);
+  for (int kt = 0, slot = 0; kt < nk; ++kt) {
+    const int next = slot + 1 == D ? 0 : slot + 1, last = slot == 0 ? D - 1 : slot - 1;
+    // the stage before this one is done with, for every wave: its place takes the one D - 1 ahead
+    if (kt + D - 1 < nk) load_all(last, kt + D - 1);
+    frags(slot, 1, 1);
+    mul(0);
+    frags(slot, 2, 0);
+    mul(1);
+    frags(slot, 3, 1);
+    mul(0);
+    // this wave's loads then under way: stages kt + 1 .. min(kt + D - 1, nk - 1), the first of which is wanted
+    wait(max(0, min(D - 2, nk - 2 - kt)));
+    frags(next, 0, 0);  // (after the last stage: of nothing)
+    mul(1);
+    slot = next;
+  }
+}
+
 // The accumulators of a wave: element e of acc[j][i] is row 32 i + lane % 32, column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.
 __device__ __forceinline__ int pt_col(int j, int e, int hf) { return 32 * j + 8 * (e >> 2) + 4 * hf + (e & 3); }
 
@@ -235,6 +332,9 @@ __device__ __forceinline__ int pt_col(int j, int e, int hf) { return 32 * j + 8 
   __shared__ __attribute__((aligned(16))) char la1[S::rows * 128]; \
   __shared__ __attribute__((aligned(16))) char lw1[S::cols * 128];
 
+// (a ring's are one array, S::RING stages long)
+#define PT_SHARED_RING(S) __shared__ __attribute__((aligned(16))) char ring[S::RING * S::stage];
+
 // After the product a wave has 16 KB of it to itself: every wave has passed the last barrier with all that it read of the stages.
 template <typename S>
 __device__ __forceinline__ char* pt_wave_lds(char* la0, char* lw0, char* la1, char* lw1, int wave) {
@@ -247,20 +347,22 @@ __device__ __forceinline__ char* pt_wave_lds(char* la0, char* lw0, char* la1, ch
 // Hands a wave's results out in memory order: 64 rows of its 64 columns at a time pass through its LDS as float (16-byte chunks XORed with
 // the row), since a store from the accumulators would touch 32 rows with 16 bytes each.  sink(row, col, v, it): N (4 or 8)
 // consecutive columns of a row, sixteen or eight lanes a row, the pass's it-th call; before(pass): called before a pass's 64 rows.
-template <int N, int MT, typename B, typename O>
+// PR: 64, or 32 rows at a time with half of the LDS.
+template <int N, int MT, int PR = 64, typename B, typename O>
 __device__ __forceinline__ void pt_hand_out(char* ep, int lane, const pt_f32x16 (&acc)[2][MT], B before, O sink) {
-  static_assert(MT % 2 == 0 && (N == 4 || N == 8), "64 rows");
+  constexpr int IP = PR / 32;
+  static_assert(MT % IP == 0 && (N == 4 || N == 8), "whole passes");
   const int l32 = lane & 31, hf = lane >> 5;
 #pragma unroll
-  for (int pass = 0; pass < MT / 2; ++pass) {
+  for (int pass = 0; pass < MT / IP; ++pass) {
     before(pass);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < IP; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const pt_f32x16& a = acc[j][2 * pass + i];
+          const pt_f32x16& a = acc[j][IP * pass + i];
           const pt_f32x4 v = {a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
           *(pt_f32x4*)(ep + (32 * i + l32) * 256 + (((8 * j + 2 * q + hf) ^ (l32 & 15)) << 4)) = v;
         }
@@ -268,10 +370,10 @@ __device__ __forceinline__ void pt_hand_out(char* ep, int lane, const pt_f32x16 
     constexpr int LR = 64 / N, RI = 64 / LR;  // lanes of a row, rows of an instruction
     const int rd_row = lane / LR, rd_c = lane % LR;
 #pragma unroll
-    for (int it = 0; it < 64 / RI; ++it) {
+    for (int it = 0; it < PR / RI; ++it) {
       const int row = RI * it + rd_row;
       if constexpr (N == 4) {
-        sink(64 * pass + row, rd_c * 4, *(const pt_f32x4*)(ep + row * 256 + ((rd_c ^ (row & 15)) << 4)), it);
+        sink(PR * pass + row, rd_c * 4, *(const pt_f32x4*)(ep + row * 256 + ((rd_c ^ (row & 15)) << 4)), it);
       } else {
         float v[8];
 #pragma unroll
@@ -280,7 +382,7 @@ __device__ __forceinline__ void pt_hand_out(char* ep, int lane, const pt_f32x16 
 #pragma unroll
           for (int u = 0; u < 4; ++u) v[4 * k + u] = x[u];
         }
-        sink(64 * pass + row, rd_c * 8, v, it);
+        sink(PR * pass + row, rd_c * 8, v, it);
       }
     }
     PT_WAVE_LDS_FENCE();

@@ -68,10 +68,10 @@ def test_other_numbers_of_steps(steps):
 def test_a_batch_is_its_matrices():
     """Also more of them than go together, and bfloat16 and in place."""
     import torch
-    x = torch.stack([torch.from_numpy(_matrix(70, 130, "low", i)) for i in range(27)]).to("cuda", torch.bfloat16)
+    x = torch.stack([torch.from_numpy(_matrix(70, 130, "low", i)) for i in range(51)]).to("cuda", torch.bfloat16)
     one = torch.stack([P.orthogonalize(m) for m in x])
     assert (P.orthogonalize(x) == one).all()
-    assert _off(one[26].double().cpu().numpy(), newton_schulz(x[26].double().cpu().numpy())) <= 4e-3
+    assert _off(one[50].double().cpu().numpy(), newton_schulz(x[50].double().cpu().numpy())) <= 4e-3
     y = x.clone()
     assert P.orthogonalize(y, out=y) is y and (y == one).all()
     assert P.orthogonalize(x[:0]).shape == (0, 70, 130)
@@ -110,7 +110,7 @@ def _np(ts):
 def test_step_against_the_oracle(nesterov):
     """More tensors than go together, of all orientations, one of them empty; the parameters' move is compared, 2-norm."""
     import torch
-    shapes = [(64, 64), (128, 40), (40, 128), (0, 5), (1, 33), (33, 1), (192, 64), (65, 200)] * 4
+    shapes = [(64, 64), (128, 40), (40, 128), (0, 5), (1, 33), (33, 1), (192, 64), (65, 200)] * 7
     p, grad, m, b = _tensors(shapes, 3)
     p0, g0, m0 = _np(p), _np(grad), _np(m)
     kw = dict(lr=0.05, momentum=0.9, nesterov=nesterov, weight_decay=0.1, rms=0.3, grad_scale=0.5)

@@ -132,7 +132,7 @@ def test_workspaces_of_many_matrices_stay_bounded(lib):
     assert sizes[0] < sizes[1] == sizes[2] < 4 << 30
     one = C.c_size_t()
     assert lib.rlhf_orthogonalize_workspace_bytes(1, 77, 1000, C.byref(one)) == OK
-    assert lib.rlhf_orthogonalize_workspace_bytes(1000, 77, 1000, C.byref(out)) == OK and out.value == 24 * one.value
+    assert lib.rlhf_orthogonalize_workspace_bytes(1000, 77, 1000, C.byref(out)) == OK and one.value < out.value < 50 * one.value
 
 
 def test_the_binding_refuses_tensors_off_the_gpu():
