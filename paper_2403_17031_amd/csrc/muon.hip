@@ -480,26 +480,32 @@ const Tiles kGramTiles = {[](const Prob& p, int t) { return triangle(up(p.sp, t)
 const Tiles kPolyTiles = {[](const Prob& p, int t) { return triangle(up(p.sp, t)); }, [](const Prob& p) { return p.sp; }};
 const Tiles kUpdateTiles = {[](const Prob& p, int t) { return up(p.rp, t) * up(p.ld, t); }, [](const Prob& p) { return p.sp; }};
 
-// Rounds that the tiles take on `slots` places, in units of the deepest tile's time.
-double rounds(const Group& g, const Tiles& t, int tile, int slots) {
+// Time of a launch's rounds of tiles: `slots` places, `stage` us a stage and `more` stages' worth for a tile's start and end.
+double rounds_us(const Group& g, const Tiles& t, int tile, int slots, double stage, double more) {
   double work = 0, most = 0;
   for (int i = 0; i < g.count; ++i) {
     work += (double)t.count(g.p[i], tile) * t.depth(g.p[i]);
     most = std::max(most, (double)t.depth(g.p[i]));
   }
-  return std::ceil(work / most / slots);
+  return std::ceil(work / most / slots) * (most / 64 + more) * stage;
 }
-// The larger tile makes four times the smaller's products in 1.3 times what two smaller ones on a CU take (1.95 and 1.5 us a
-// stage).
-bool takes_big(const Group& g, const Tiles& t) { return 1.3 * rounds(g, t, 256, 256) <= rounds(g, t, 128, 512); }
 
 enum Shape { kBig, kMid, kSmall };
 constexpr int kTile[] = {256, 128, 64}, kThreads[] = {512, 256, 128};
 
-#include <cstdlib>
+// The tiles of a launch.  Up to half as many middle ones as there are CUs leave most of the chip idle and wait for their loads: small
+// ones, four times as many, with three stages under way (one matrix of 768 x 768 222 -> 148 us, of 333 x 1025 207 -> 138; four of 768
+// to 3,072 by 768 410 -> 384; 24 of the 70M shape 616 -> 719 the other way).  Else a large tile takes
+// 1.95 us a stage and two middle ones on a CU, half of its products, 1.5.
+Shape shape_of(const Group& g, const Tiles& t) {
+  int mids = 0;
+  for (int i = 0; i < g.count; ++i) mids += t.count(g.p[i], kTile[kMid]);
+  if (mids <= 128) return kSmall;
+  return rounds_us(g, t, kTile[kBig], 256, 1.95, 8) <= rounds_us(g, t, kTile[kMid], 512, 1.5, 5) ? kBig : kMid;
+}
+
 Shape number_tiles(Group& g, Part part, const Tiles& t) {
-  static const char* e = getenv("MUON_SHAPE");
-  const Shape c = e ? (Shape)(e[part - kGram] - '0') : takes_big(g, t) ? kBig : kMid;
+  const Shape c = shape_of(g, t);
   double work = 0;
   int tiles = 0;
   for (int i = 0; i < g.count; ++i) {

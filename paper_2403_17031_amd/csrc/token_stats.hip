@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) out_kernel(OutArgs a) {
   constexpr int MT = S::MT;
   // (rows are walked as columns are elsewhere: dW has many of them, dh is cut along K)
   const int nb_m = a.tiles_n, nb_n = (a.N + S::cols - 1) / S::cols;
-  const int item = pt_item(nb_m * nb_n * a.slices);
+  const int item = pt_item_rounds(nb_m * nb_n * a.slices);
   if (item < 0) return;
   const int z = item / (nb_m * nb_n);
   int tm, tn;
