@@ -269,10 +269,11 @@ int rlhf_token_stats_backward(const void *hidden, int64_t ld_hidden, const void 
 /* Orthogonalisation by Newton-Schulz products, of `batch` matrices [rows, cols] one after the other in memory:
  *   X = x / (|x|_F + eps);  ns_steps times  A = X X^T,  X <- a X + (b A + c A^2) X;  (a, b, c) = (3.4445, -4.7750, 2.0315)
  * (the coefficients that the Muon optimiser published; from the other side where rows > cols), out = X: singular values of
- * a thousandth of the norm and more come to lie between 0.7 and 1.2 in five steps.  x: dev float or bfloat16 (dtype); out: dev
+ * 0.0015 of the norm and more come to lie between 0.68 and 1.21 in five steps.  x: dev float or bfloat16 (dtype); out: dev
  * bfloat16, may be x.  The products take fp16 operands with fp32 sums, X itself is kept in 22 bits: results are within 0.4 % of
  * the iteration in exact arithmetic (2-norm, five steps), rounding to bfloat16 included.  1 <= ns_steps <= 16; the shorter side at
- * most 32,768, the longer at most 1,048,576. */
+ * most 32,768, the longer at most 1,048,576, elements at most 2^31 - 1.  A matrix that holds infinities or NaN becomes NaN; the others
+ * of a call do not notice. */
 int rlhf_orthogonalize_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, size_t *out);
 int rlhf_orthogonalize(const void *x, int32_t dtype, int32_t batch, int32_t rows, int32_t cols, int32_t ns_steps, double eps,
                        uint16_t *out, void *workspace, size_t workspace_bytes, void *stream);

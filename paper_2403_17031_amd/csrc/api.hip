@@ -964,7 +964,8 @@ int rlhf_token_stats(const void* hidden, int64_t ld_hidden, const void* weight, 
   if (!hidden || !weight || !targets || !out_logprobs || !out_entropy || !out_lse || !workspace)
     return fail(RLHF_EINVAL, "null pointer argument");
   if (top_k > 0 && (!out_top_ids || !out_top_logprobs)) return fail(RLHF_EINVAL, "top_k > 0 needs both of its outputs");
-  if (!(temperature > 0.f) || !std::isfinite(temperature)) return fail(RLHF_EINVAL, "temperature must be finite and > 0");
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
+    return fail(RLHF_EINVAL, "temperature and its reciprocal must be finite and > 0");
   if ((((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)workspace) & 15) != 0)
     return fail(RLHF_EINVAL, "matrices and workspace must be 16-byte aligned");
   if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_token_stats_workspace_bytes reports");
@@ -1016,7 +1017,8 @@ int rlhf_token_stats_backward(const void* hidden, int64_t ld_hidden, const void*
   if (const int rc = rlhf_token_stats_backward_workspace_bytes(T, d, V, ld_hidden, ld_weight, dtype, grad_dtype, &need)) return rc;
   if (!hidden || !weight || !targets || !lse || !d_logprobs || !d_hidden || !d_weight || !workspace || (d_entropy && !entropy))
     return fail(RLHF_EINVAL, "null pointer argument");
-  if (!(temperature > 0.f) || !std::isfinite(temperature)) return fail(RLHF_EINVAL, "temperature must be finite and > 0");
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
+    return fail(RLHF_EINVAL, "temperature and its reciprocal must be finite and > 0");
   if ((((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)workspace) & 15) != 0)
     return fail(RLHF_EINVAL, "matrices and workspace must be 16-byte aligned");
   if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_token_stats_backward_workspace_bytes reports");
@@ -1039,8 +1041,8 @@ int rlhf_token_stats_backward(const void* hidden, int64_t ld_hidden, const void*
 
 // ---- orthogonalised updates ----
 static int check_muon_shape(int32_t rows, int32_t cols) {
-  if (std::min(rows, cols) > 32768 || std::max(rows, cols) > (1 << 20))
-    return fail(RLHF_EUNSUPPORTED, "a matrix's shorter side may have 32,768 entries, its longer 1,048,576");
+  if (std::min(rows, cols) > 32768 || std::max(rows, cols) > (1 << 20) || (int64_t)rows * cols > INT32_MAX)
+    return fail(RLHF_EUNSUPPORTED, "a matrix's shorter side may have 32,768 entries, its longer 1,048,576, all of it 2^31 - 1");
   return RLHF_OK;
 }
 static int check_ns(int32_t ns_steps, double eps) {
@@ -1073,7 +1075,7 @@ int rlhf_orthogonalize(const void* x, int32_t dtype, int32_t batch, int32_t rows
   MuonScalars c = {};
   c.src_bf16 = dtype == RLHF_DTYPE_BF16;
   c.steps = ns_steps;
-  c.eps = (float)eps;
+  c.eps = eps;
   const size_t n = (size_t)rows * cols;
   for (int32_t from = 0; from < batch; from += kMuonGroup) {
     MuonMatrix ms[kMuonGroup] = {};
@@ -1150,7 +1152,7 @@ int rlhf_muon_step(const rlhf_muon_tensor* tensors, int32_t count, double lr, do
   c.beta = (float)momentum;
   c.omb = (float)(1.0 - momentum);
   c.grad_scale = (float)grad_scale;
-  c.eps = (float)eps;
+  c.eps = eps;
   c.decay = (float)(1.0 - lr * weight_decay);
   c.lr_rms = lr * rms;
   MuonMatrix ms[kMuonGroup];

@@ -19,9 +19,8 @@ struct MuonMatrix {
 struct MuonScalars {
   int src_bf16, nesterov, steps;
   float beta, omb, grad_scale;  // moment = beta moment + omb grad_scale grad
-  float eps;
   float decay;                  // param = decay param - lr rms sqrt(max(rows, cols)) O
-  double lr_rms;
+  double lr_rms, eps;
 };
 constexpr int kMuonGroup = 48;  // most matrices of a call
 // Workspace bytes of a call on matrices of these sizes.

@@ -1,7 +1,7 @@
 // Orthogonalised updates.  A matrix G is brought towards the orthogonal factor of its singular value decomposition by the quintic
 // Newton-Schulz iteration: X = G / (|G|_F + eps), then `steps` times
 //   A = X X^T,  B = b A + c A^2,  X <- a X + B X      (a, b, c = 3.4445, -4.7750, 2.0315)
-// which maps each singular value s to a s + b s^3 + c s^5 and brings those of 1e-3 and more near 1 in five steps.  A matrix
+// which maps each singular value s to a s + b s^3 + c s^5 and brings those of 0.0015 and more to 0.68 .. 1.21 in five.  A matrix
 // with more rows than columns is taken from the other side, A = X^T X and X <- a X + X B, in its own layout: which side of a
 // product an operand stands on is a matter of reading it row-major or K-major.
 //
@@ -37,13 +37,17 @@ __device__ __forceinline__ char* muon_wave_lds(char* ring, char* la0, char* lw0,
   if constexpr (S::RING > 2) return ring + wave * 16384;
   else return pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
 }
-// One tile's product, whichever way the shape keeps its stages, and the LDS a wave has afterwards.
-#define MUON_LDS(S) __shared__ __attribute__((aligned(16))) char lds[S::RING > 2 ? S::RING * S::stage : 16];          \
-  __shared__ __attribute__((aligned(16))) char la0[S::RING > 2 ? 16 : S::rows * 128], lw0[S::RING > 2 ? 16 : S::cols * 128]; \
-  __shared__ __attribute__((aligned(16))) char la1[S::RING > 2 ? 16 : S::rows * 128], lw1[S::RING > 2 ? 16 : S::cols * 128];
-#define MUON_WAVE_LDS muon_wave_lds<S>(lds, la0, lw0, la1, lw1)
-#define MUON_PRODUCT(AK, WK, ...)                                                               \
-  if constexpr (S::RING > 2) pt_product_ring<half_t, AK, WK, S>(__VA_ARGS__, lds, acc);         \
+// One tile's product into acc, whichever way the shape keeps its stages, and the LDS a wave has afterwards.
+#define MUON_LDS(S)                                                                                     \
+  constexpr bool kRing = S::RING > 2;                                                                   \
+  __shared__ __attribute__((aligned(16))) char ring[kRing ? S::RING * S::stage : 16];                   \
+  __shared__ __attribute__((aligned(16))) char la0[kRing ? 16 : S::rows * 128];                         \
+  __shared__ __attribute__((aligned(16))) char lw0[kRing ? 16 : S::cols * 128];                         \
+  __shared__ __attribute__((aligned(16))) char la1[kRing ? 16 : S::rows * 128];                         \
+  __shared__ __attribute__((aligned(16))) char lw1[kRing ? 16 : S::cols * 128];
+#define MUON_WAVE_LDS muon_wave_lds<S>(ring, la0, lw0, la1, lw1)
+#define MUON_PRODUCT(AK, WK, ...)                                                     \
+  if constexpr (kRing) pt_product_ring<half_t, AK, WK, S>(__VA_ARGS__, ring, acc);    \
   else pt_product<half_t, AK, WK, S>(__VA_ARGS__, la0, lw0, la1, lw1, acc)
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
@@ -218,7 +222,10 @@ __global__ void __launch_bounds__(256) muon_scale_kernel(const Group* __restrict
     if ((int)threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
     __syncthreads();
   }
-  if (threadIdx.x == 0) *p.scale = (float)((double)kXScale / (sqrt(sh[0]) + (double)c.eps));
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(sh[0]) + c.eps;
+    *p.scale = norm != norm ? NAN : (float)fmin((double)kXScale / norm, 3e38);  // (finite, so that nothing stays 0)
+  }
 }
 
 // X = scale * source as two halves, zero in the padding; eight columns a thread.
@@ -306,8 +313,7 @@ __global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_gram_
     MUON_PRODUCT(true, true, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp);
   else
     MUON_PRODUCT(false, false, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld);
-  store_symmetric<S, false>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f,
-                     MUON_WAVE_LDS);
+  store_symmetric<S, false>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f, MUON_WAVE_LDS);
 }
 
 // B = b A + c A^2
@@ -322,8 +328,7 @@ __global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_poly_
   if (tm * S::rows >= p.sp) return;
   pt_f32x16 acc[S::NT][S::MT];
   MUON_PRODUCT(false, false, p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp);
-  store_symmetric<S, true>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB,
-                     MUON_WAVE_LDS);
+  store_symmetric<S, true>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB, MUON_WAVE_LDS);
 }
 
 // X <- a X + B X, or after the last step what becomes of it
@@ -494,9 +499,9 @@ enum Shape { kBig, kMid, kSmall };
 constexpr int kTile[] = {256, 128, 64}, kThreads[] = {512, 256, 128};
 
 // The tiles of a launch.  Up to half as many middle ones as there are CUs leave most of the chip idle and wait for their loads: small
-// ones, four times as many, with three stages under way (one matrix of 768 x 768 222 -> 148 us, of 333 x 1025 207 -> 138; four of 768
-// to 3,072 by 768 410 -> 384; 24 of the 70M shape 616 -> 719 the other way).  Else a large tile takes
-// 1.95 us a stage and two middle ones on a CU, half of its products, 1.5.
+// ones, four times as many, with three stages under way (one matrix of 768 x 768 225 -> 149 us, of 333 x 1025 213 -> 138, the four of a
+// layer of width 768 410 -> 337; 24 of the 70M shape 616 -> 719 the other way).  Else a large tile takes 1.95 us a stage and two
+// middle ones on a CU, half of its products, 1.5.
 Shape shape_of(const Group& g, const Tiles& t) {
   int mids = 0;
   for (int i = 0; i < g.count; ++i) mids += t.count(g.p[i], kTile[kMid]);

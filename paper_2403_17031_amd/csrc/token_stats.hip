@@ -639,8 +639,15 @@ __global__ void __launch_bounds__(256) out_sum_kernel(OutArgs a) {
   if (i >= (size_t)a.M * quads) return;
   const int row = (int)(i / quads), col = (int)(i - (size_t)row * quads) * 4;
   const float* const p = a.slab + (size_t)row * a.lds + col;
-  pt_f32x4 v = *(const pt_f32x4*)p;
-  for (int z = 1; z < a.slices; ++z) v += *(const pt_f32x4*)(p + (size_t)z * a.M * a.lds);
+  pt_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int z0 = 0; z0 < a.slices; z0 += 8) {  // (eight loads under way)
+    pt_f32x4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = *(const pt_f32x4*)(p + (size_t)min(z0 + k, a.slices - 1) * a.M * a.lds);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (z0 + k < a.slices) v += x[k];
+  }
   const float s = a.scale ? a.scale[1] : 1.f;
 #pragma unroll
   for (int u = 0; u < 4; ++u) v[u] *= s;
@@ -809,7 +816,7 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
     };
     // rows of a finishing block: many share the lines of the parts' sums, few leave no CU idle
     if (n >= 4096 && finish_lds(parts, 8, a.top) <= 60 * 1024) finish(std::integral_constant<int, 8>{});
-    else if (n >= 1024 && finish_lds(parts, 4, a.top) <= 60 * 1024) finish(std::integral_constant<int, 4>{});
+    else if (n >= 512 && finish_lds(parts, 4, a.top) <= 60 * 1024) finish(std::integral_constant<int, 4>{});
     else finish(std::integral_constant<int, 1>{});
     if ((*err = hipGetLastError()) != hipSuccess) return ws.off;
   }

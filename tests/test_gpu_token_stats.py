@@ -118,6 +118,37 @@ def test_equal_logits_go_to_the_lower_id():
     assert torch.allclose(neg["entropy"], torch.full((T,), float(np.log(1000.0)), device="cuda"), rtol=1e-6)
 
 
+@pytest.mark.parametrize("T,V,k", [(3, 5000, 20), (2, 5000, 50), (2, 300, 64), (2816, 50304, 8)])
+def test_more_equal_logits_than_the_quick_way_holds(T, V, k):
+    """All logits equal but one, last: its id first, then the lowest."""
+    import torch
+    h = torch.ones(T, 64, device="cuda", dtype=torch.bfloat16)
+    w = torch.zeros(V, 64, device="cuda", dtype=torch.bfloat16)
+    w[V - 1] = 0.25
+    got = P.token_stats(h, w, torch.full((T,), V - 1, dtype=torch.int32, device="cuda"), 0.7, k)
+    want = torch.tensor([V - 1] + list(range(k - 1)), dtype=torch.int32, device="cuda")
+    assert (got["top_ids"] == want).all()
+    lse = np.log((V - 1) + np.exp(16 / 0.7))
+    assert float((got["logprobs"] - (16 / 0.7 - lse)).abs().max()) <= 1e-4 and float((got["top_logprobs"][:, 1:] + lse).abs().max()) <= 1e-4
+
+
+@pytest.mark.parametrize("k", [1, 8, 24, 40])
+def test_rows_enough_for_part_of_the_logits_to_be_kept(k):
+    """2,816 rows of 50,304 entries: after an eighth of the vocabulary only parts that can hold an alternative are stored."""
+    import torch
+    h, w, y, th, tw, ty = _inputs(2816, 64, 50304, "bf16", 5, lean=0.5)
+    got = P.token_stats(th, tw, ty, 0.7, k)
+    plain = P.token_stats(th, tw, ty, 0.7)
+    logits = (th.double() @ tw.double().T)
+    order = torch.sort(logits, dim=1, descending=True, stable=True)
+    assert (got["top_ids"] == order.indices[:, :k]).all()
+    lse = torch.logsumexp(logits / 0.7, 1)
+    tol = 2.0**-22 * float(logits.abs().max()) / 0.7 + 2.0**-21 + 900 * 2.0**-24
+    assert ((got["top_logprobs"] - (order.values[:, :k] / 0.7 - lse[:, None])).abs() <= 2 * tol).all()
+    for n in plain:
+        assert (got[n] == plain[n]).all(), n
+
+
 def test_one_sure_token_and_large_logits():
     """A token that has everything: its log-probability and the entropy are 0, not NaN; others' log-probabilities are their distance."""
     import torch

@@ -30,7 +30,7 @@ def _stats(lib, **over):
     (dict(ent=None), EINVAL), (dict(lse=None), EINVAL), (dict(ids=None), EINVAL), (dict(tlp=None), EINVAL), (dict(ws=None), EINVAL),
     (dict(temp=0.0), EINVAL), (dict(temp=-1.0), EINVAL), (dict(temp=float("nan")), EINVAL), (dict(temp=float("inf")), EINVAL),
     (dict(h=PTR + 8), EINVAL), (dict(w=PTR + 2), EINVAL), (dict(ws=PTR + 4), EINVAL), (dict(n=0), ENOMEM),
-    (dict(ldh=1 << 23), EUNSUPPORTED), (dict(T=(1 << 26) + 1), EUNSUPPORTED),
+    (dict(temp=1e-39), EINVAL), (dict(ldh=1 << 23), EUNSUPPORTED), (dict(T=(1 << 26) + 1), EUNSUPPORTED),
 ])
 def test_token_stats_refusals(lib, over, rc):
     assert _stats(lib, **over) == rc and lib.rlhf_last_error()
@@ -77,7 +77,7 @@ def _orth(lib, **over):
     (dict(batch=0), EINVAL), (dict(rows=0), EINVAL), (dict(cols=-3), EINVAL), (dict(x=None), EINVAL), (dict(out=None), EINVAL),
     (dict(ws=None), EINVAL), (dict(dtype=2), EUNSUPPORTED), (dict(steps=0), EINVAL), (dict(steps=17), EINVAL), (dict(eps=0.0), EINVAL),
     (dict(eps=float("nan")), EINVAL), (dict(n=0), ENOMEM), (dict(rows=32769, cols=32769), EUNSUPPORTED),
-    (dict(rows=(1 << 20) + 1, cols=1), EUNSUPPORTED), (dict(x=PTR + 2), EINVAL), (dict(ws=PTR + 8), EINVAL),
+    (dict(rows=(1 << 20) + 1, cols=1), EUNSUPPORTED), (dict(rows=1 << 17, cols=1 << 14), EUNSUPPORTED), (dict(x=PTR + 2), EINVAL), (dict(ws=PTR + 8), EINVAL),
 ])
 def test_orthogonalize_refusals(lib, over, rc):
     assert _orth(lib, **over) == rc and lib.rlhf_last_error()
