@@ -27,29 +27,6 @@ namespace rlhf {
 
 namespace {
 
-using PtBig = PtShape<2, 4, 4, 2>;
-using PtMid = PtShape<2, 2, 2, 2>;
-using PtSmall = PtShape<2, 1, 1, 2, 4>;  // 64 x 64, two waves, a ring of four stages
-
-template <typename S>
-__device__ __forceinline__ char* muon_wave_lds(char* ring, char* la0, char* lw0, char* la1, char* lw1) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if constexpr (S::RING > 2) return ring + wave * 16384;
-  else return pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
-}
-// One tile's product into acc, whichever way the shape keeps its stages, and the LDS a wave has afterwards.
-#define MUON_LDS(S)                                                                                     \
-  constexpr bool kRing = S::RING > 2;                                                                   \
-  __shared__ __attribute__((aligned(16))) char ring[kRing ? S::RING * S::stage : 16];                   \
-  __shared__ __attribute__((aligned(16))) char la0[kRing ? 16 : S::rows * 128];                         \
-  __shared__ __attribute__((aligned(16))) char lw0[kRing ? 16 : S::cols * 128];                         \
-  __shared__ __attribute__((aligned(16))) char la1[kRing ? 16 : S::rows * 128];                         \
-  __shared__ __attribute__((aligned(16))) char lw1[kRing ? 16 : S::cols * 128];
-#define MUON_WAVE_LDS muon_wave_lds<S>(ring, la0, lw0, la1, lw1)
-#define MUON_PRODUCT(AK, WK, ...)                                                     \
-  if constexpr (kRing) pt_product_ring<half_t, AK, WK, S>(__VA_ARGS__, ring, acc);    \
-  else pt_product<half_t, AK, WK, S>(__VA_ARGS__, la0, lw0, la1, lw1, acc)
-
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kXScale = 2048.f, kAScale = 4096.f;
 constexpr int kProbs = kMuonGroup;  // of a launch
@@ -292,15 +269,15 @@ __device__ __forceinline__ void store_symmetric(pt_f32x16 (&acc)[S::NT][S::MT], 
     pt_hand_out_transposed<MT>(ep, lane, acc, [&](int c, int r, pt_u32x4 v) {
       if (row0 + r < ld) *(pt_u32x4*)(out + (size_t)(col0 + c) * ld + row0 + r) = v;
     });
-  pt_hand_out<8, MT, (MT > 1 ? 64 : 32)>(ep, lane, acc, PtNothing(), [&](int r, int c, const float(&v)[8], int) {
+  pt_hand_out<8, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, const float(&v)[8], int) {
     if (row0 + r < ld) *(pt_u32x4*)(out + (size_t)(row0 + r) * ld + col0 + c) = pt_pack8<half_t>(v);
   });
 }
 
 // A = X X^T (the shorter side's), scaled
 template <typename S>
-__global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_gram_kernel(const Group* __restrict__ g, int cur) {
-  MUON_LDS(S)
+__global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_gram_kernel(const Group* __restrict__ g, int cur) {
+  PT_LDS(S)
   int tile;
   const Prob& p = find_tile(g, kGram, tile);
   if (tile < 0) return;
@@ -310,16 +287,16 @@ __global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_gram_
   pt_f32x16 acc[S::NT][S::MT];
   const half_t* const x = p.xh[cur];
   if (p.m.rows > p.m.cols)
-    MUON_PRODUCT(true, true, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp);
+    PT_PRODUCT(half_t, true, true, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp);
   else
-    MUON_PRODUCT(false, false, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld);
-  store_symmetric<S, false>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f, MUON_WAVE_LDS);
+    PT_PRODUCT(half_t, false, false, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld);
+  store_symmetric<S, false>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f, PT_WAVE_LDS);
 }
 
 // B = b A + c A^2
 template <typename S>
-__global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_poly_kernel(const Group* __restrict__ g) {
-  MUON_LDS(S)
+__global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_poly_kernel(const Group* __restrict__ g) {
+  PT_LDS(S)
   int tile;
   const Prob& p = find_tile(g, kPoly, tile);
   if (tile < 0) return;
@@ -327,15 +304,15 @@ __global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_poly_
   pt_tile_triangle(tile, tm, tn);
   if (tm * S::rows >= p.sp) return;
   pt_f32x16 acc[S::NT][S::MT];
-  MUON_PRODUCT(false, false, p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp);
-  store_symmetric<S, true>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB, MUON_WAVE_LDS);
+  PT_PRODUCT(half_t, false, false, p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp);
+  store_symmetric<S, true>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB, PT_WAVE_LDS);
 }
 
 // X <- a X + B X, or after the last step what becomes of it
 template <typename S>
-__global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_update_kernel(const Group* __restrict__ g, int cur, int last) {
+__global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_update_kernel(const Group* __restrict__ g, int cur, int last) {
   const MuonScalars c = g->c;
-  MUON_LDS(S)
+  PT_LDS(S)
   constexpr int MT = S::MT;
   int tile;
   const Prob& p = find_tile(g, kUpdate, tile);
@@ -345,9 +322,9 @@ __global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_updat
   pt_tile_pos(tile, nb_m, nb_n, tm, tn);
   pt_f32x16 acc[2][MT];
   if (p.m.rows > p.m.cols)
-    MUON_PRODUCT(false, false, p.xh[cur], p.ld, tm * S::rows, p.rp, p.b, p.sp, tn * S::cols, p.sp, 0, p.sp);
+    PT_PRODUCT(half_t, false, false, p.xh[cur], p.ld, tm * S::rows, p.rp, p.b, p.sp, tn * S::cols, p.sp, 0, p.sp);
   else
-    MUON_PRODUCT(false, true, p.b, p.sp, tm * S::rows, p.sp, p.xh[cur], p.ld, tn * S::cols, p.ld, 0, p.sp);
+    PT_PRODUCT(half_t, false, true, p.b, p.sp, tm * S::rows, p.sp, p.xh[cur], p.ld, tn * S::cols, p.ld, 0, p.sp);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -361,8 +338,8 @@ __global__ void __launch_bounds__(64 * S::waves, S::RING > 2 ? 1 : 2) muon_updat
   half_t* const nl = p.xl[cur ^ 1] + (size_t)row0 * p.ld + col0;
   f16x8 h[MT > 1 ? 8 : 4], l[MT > 1 ? 8 : 4];  // this pass's X, requested before the results go through LDS
   constexpr int PR = MT > 1 ? 64 : 32, NI = PR / 8;
-  pt_hand_out<8, MT, PR>(
-      MUON_WAVE_LDS, lane, acc,
+  pt_hand_out<8, MT>(
+      PT_WAVE_LDS, lane, acc,
       [&](int pass) {
 #pragma unroll
         for (int it = 0; it < NI; ++it) {

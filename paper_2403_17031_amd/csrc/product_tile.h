@@ -325,16 +325,6 @@ __device__ __forceinline__ int pt_col(int j, int e, int hf) { return 32 * j + 8 
   __builtin_amdgcn_wave_barrier();                   \
   __builtin_amdgcn_sched_barrier(0);
 
-// The stages' LDS of a block: operands of stage 0 and of stage 1 (see pt_product).
-#define PT_SHARED(S)                                               \
-  __shared__ __attribute__((aligned(16))) char la0[S::rows * 128]; \
-  __shared__ __attribute__((aligned(16))) char lw0[S::cols * 128]; \
-  __shared__ __attribute__((aligned(16))) char la1[S::rows * 128]; \
-  __shared__ __attribute__((aligned(16))) char lw1[S::cols * 128];
-
-// (a ring's are one array, S::RING stages long)
-#define PT_SHARED_RING(S) __shared__ __attribute__((aligned(16))) char ring[S::RING * S::stage];
-
 // After the product a wave has 16 KB of it to itself: every wave has passed the last barrier with all that it read of the stages.
 template <typename S>
 __device__ __forceinline__ char* pt_wave_lds(char* la0, char* lw0, char* la1, char* lw1, int wave) {
@@ -344,13 +334,40 @@ __device__ __forceinline__ char* pt_wave_lds(char* la0, char* lw0, char* la1, ch
   return base + wave % per * 16384;
 }
 
+template <typename S>
+__device__ __forceinline__ char* pt_any_wave_lds(char* ring, char* la0, char* lw0, char* la1, char* lw1) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if constexpr (S::RING > 2) return ring + wave * 16384;
+  else return pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
+}
+
+// One tile's product into acc, whichever way the shape keeps its stages (a ring's are one array), and the LDS a wave has afterwards.
+#define PT_LDS(S)                                                                     \
+  constexpr bool kRing = S::RING > 2;                                                 \
+  __shared__ __attribute__((aligned(16))) char ring[kRing ? S::RING * S::stage : 16]; \
+  __shared__ __attribute__((aligned(16))) char la0[kRing ? 16 : S::rows * 128];       \
+  __shared__ __attribute__((aligned(16))) char lw0[kRing ? 16 : S::cols * 128];       \
+  __shared__ __attribute__((aligned(16))) char la1[kRing ? 16 : S::rows * 128];       \
+  __shared__ __attribute__((aligned(16))) char lw1[kRing ? 16 : S::cols * 128];
+#define PT_WAVE_LDS pt_any_wave_lds<S>(ring, la0, lw0, la1, lw1)
+#define PT_PRODUCT(T, AK, WK, ...)                                            \
+  if constexpr (kRing) pt_product_ring<T, AK, WK, S>(__VA_ARGS__, ring, acc); \
+  else pt_product<T, AK, WK, S>(__VA_ARGS__, la0, lw0, la1, lw1, acc)
+
+// The shapes in use.
+using PtBig = PtShape<2, 4, 4, 2>;       // 256 x 256, 8 waves of 128 x 64, a CU to itself
+using PtMid = PtShape<2, 2, 2, 2>;       // 128 x 128, 4 waves of 64 x 64, two blocks on a CU
+using PtSmall = PtShape<2, 1, 1, 2, 4>;  // 64 x 64, 2 waves of 32 x 64, a ring of four stages, two blocks on a CU
+template <typename S>
+constexpr int pt_waves_eu = S::RING > 2 ? 1 : 2;  // for __launch_bounds__
+
 // Hands a wave's results out in memory order: 64 rows of its 64 columns at a time pass through its LDS as float (16-byte chunks XORed with
 // the row), since a store from the accumulators would touch 32 rows with 16 bytes each.  sink(row, col, v, it): N (4 or 8)
 // consecutive columns of a row, sixteen or eight lanes a row, the pass's it-th call; before(pass): called before a pass's 64 rows.
-// PR: 64, or 32 rows at a time with half of the LDS.
-template <int N, int MT, int PR = 64, typename B, typename O>
+// (32 rows where a wave has no more)
+template <int N, int MT, typename B, typename O>
 __device__ __forceinline__ void pt_hand_out(char* ep, int lane, const pt_f32x16 (&acc)[2][MT], B before, O sink) {
-  constexpr int IP = PR / 32;
+  constexpr int PR = MT > 1 ? 64 : 32, IP = PR / 32;
   static_assert(MT % IP == 0 && (N == 4 || N == 8), "whole passes");
   const int l32 = lane & 31, hf = lane >> 5;
 #pragma unroll

@@ -24,9 +24,6 @@ namespace rlhf {
 
 namespace {
 
-using PtBig = PtShape<2, 4, 4, 2>;  // 256 x 256, 8 waves of 128 x 64, a CU to itself (160 KB of LDS)
-using PtMid = PtShape<2, 2, 2, 2>;  // 128 x 128, 4 waves of 64 x 64, two blocks on a CU
-
 constexpr int kPart = 64;  // columns of a part
 
 __device__ __forceinline__ uint32_t order_key(float v) {  // larger for larger values, -0 as +0, NaN below all
@@ -51,8 +48,8 @@ struct StatsArgs {
 };
 
 template <typename T, typename S>
-__global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
-  PT_SHARED(S)
+__global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) stats_kernel(StatsArgs a) {
+  PT_LDS(S)
   constexpr int MT = S::MT;
   const int nb_m = (a.T + S::rows - 1) / S::rows;
   const int item = pt_item(nb_m * a.tiles_n);
@@ -61,7 +58,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
   pt_tile_pos(item, nb_m, a.tiles_n, tm, tn);
   tn += a.tile0;
   pt_f32x16 acc[2][MT];
-  pt_product<T, false, false, S>(a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, la0, lw0, la1, lw1, acc);
+  PT_PRODUCT(T, false, false, a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
@@ -84,7 +81,8 @@ __global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) m = fmaxf(m, ALL || pt_col(j, e, hf) < lim ? acc[j][i][e] : -INFINITY);
       m = half_max(m);
-      float s0 = 0.f, s1 = 0.f;
+      // s0: the sum, less: what of it is below 1 each, so without the largest entries, whose count is the difference
+      float s0 = 0.f, less = 0.f, s1 = 0.f;
       if (m > -INFINITY) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -95,6 +93,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
             if (acc[j][i][e] != acc[j][i][e]) x = acc[j][i][e];      // (the maximum passes over NaN)
             if (!ALL) x = pt_col(j, e, hf) < lim ? x : 0.f;
             s0 += x;
+            less += __builtin_amdgcn_fractf(x);
             s1 = fmaf(x, t, s1);
           }
       } else {  // -infinity alone, or NaN
@@ -105,11 +104,12 @@ __global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
             if (pt_col(j, e, hf) < lim && acc[j][i][e] != acc[j][i][e]) s0 = acc[j][i][e];
       }
       s0 = half_sum(s0);
+      less = half_sum(less);
       s1 = half_sum(s1);
       if (in && hf == 0) {
         const size_t at = (size_t)part * a.T + row;
         a.pmax[at] = m;
-        a.ps0[at] = s0;
+        a.ps0[at] = (rintf(s0 - less) - 1.f) + less;
         a.ps1[at] = s1 * 0.69314718055994531f;
       }
       if (a.thr) {  // few rows keep their part: straight from the accumulators
@@ -140,31 +140,32 @@ __global__ void __launch_bounds__(64 * S::waves, 2) stats_kernel(StatsArgs a) {
   if (a.V - col0 >= 64) sums(std::true_type{});
   else sums(std::false_type{});
   if (a.logits && !a.thr) {  // (columns up to the row stride, a multiple of 64, exist)
-    pt_hand_out<4, MT>(pt_wave_lds<S>(la0, lw0, la1, lw1, wave), lane, acc, PtNothing(), [&](int r, int c, pt_f32x4 v, int) {
+    pt_hand_out<4, MT>(PT_WAVE_LDS, lane, acc, PtNothing(), [&](int r, int c, pt_f32x4 v, int) {
       if (row0 + r < a.T) *(pt_f32x4*)(a.logits + (size_t)(row0 + r) * a.ldl + col0 + c) = v;
     });
   }
 }
 
-// (max, S0, S1) of two sets of entries
+// (max, S0 - 1, S1) of a set of entries (none: S0 = 0).  S0 is kept less the largest entry's 1, so that a token which has nearly
+// everything gets its log-probability, -log S0, to the bits of what the others have.
 struct Stat {
-  float m, s0, s1;
+  float m, over, s1;
 };
 __device__ __forceinline__ Stat stat_merge(Stat a, Stat b, float inv_t) {
-  const float m = fmaxf(a.m, b.m);
-  Stat r = {m, 0.f, 0.f};
-  auto add = [&](Stat x) {
-    if (x.m == -INFINITY) {  // nothing, or NaN alone
-      r.s0 += x.s0;
-      return;
-    }
-    const float t = (x.m - m) * inv_t, f = __expf(t);
-    r.s0 += f * x.s0;
-    r.s1 += f != 0.f ? f * (x.s1 + x.s0 * t) : 0.f;
-  };
-  add(a);
-  add(b);
-  return r;
+  if (b.m > a.m) {
+    const Stat x = a;
+    a = b;
+    b = x;
+  }
+  const float s0 = 1.f + b.over;
+  if (b.m == -INFINITY) {  // nothing, or NaN alone
+    a.over += s0;
+    return a;
+  }
+  const float t = (b.m - a.m) * inv_t, f = __expf(t);
+  a.over = fmaf(f, s0, a.over);
+  if (f != 0.f) a.s1 = fmaf(f, fmaf(s0, t, b.s1), a.s1);
+  return a;
 }
 
 // 4-byte words of LDS of a wave that looks for alternatives
@@ -239,7 +240,7 @@ constexpr int kQuickTop = 32, kQuickParts = 32;
 // False, with nothing written, where ties or an odd spread leave more than fit.
 template <int NB>
 __device__ __forceinline__ bool rank_logits(const float* logits, int V, const int* sel, int parts, int top, int lane, uint32_t* keep_key,
-                                            int* keep_col, float inv_t, float lse, int32_t* ids, float* lps) {
+                                            int* keep_col, float inv_t, float m, float ls, int32_t* ids, float* lps) {
   uint32_t x[NB], largest = 0;
   int col[NB];
 #pragma unroll
@@ -278,7 +279,7 @@ __device__ __forceinline__ bool rank_logits(const float* logits, int V, const in
   }
   if (lane < n && rank < top) {
     ids[rank] = c;
-    lps[rank] = order_value(key) * inv_t - lse;
+    lps[rank] = (order_value(key) - m) * inv_t - ls;
   }
   return true;
 }
@@ -318,13 +319,13 @@ template <int R>
 __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   __shared__ float sh[3][4][16];
-  __shared__ float row_lse[16];
+  __shared__ float row_max[16], row_log[16];
   constexpr int G = 256 / R;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = tid % R, g = tid / R, P = a.parts | 1;
   const int row = blockIdx.x * R + r;
   const bool in = row < a.T;
   uint32_t* const pm = (uint32_t*)dyn;
-  Stat s = {-INFINITY, 0.f, 0.f};
+  Stat s = {-INFINITY, -1.f, 0.f};
   if (in) {
     for (int p = g; p < a.parts; p += G) {
       const size_t at = (size_t)p * a.T + row;
@@ -346,14 +347,31 @@ __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
     return op(op(sh[k][0][r], sh[k][1][r]), op(sh[k][2][r], sh[k][3][r]));
   };
   const float m = over(s.m, [](float x, float y) { return fmaxf(x, y); }, 0);
-  s = stat_merge(s, Stat{m, 0.f, 0.f}, a.inv_t);
-  s.s0 = over(s.s0, [](float x, float y) { return x + y; }, 1);
-  s.s1 = over(s.s1, [](float x, float y) { return x + y; }, 2);
+  // the largest entry's 1 is left out once, with the first thread of the row whose own maximum it is
+  auto holder = [&] {
+    int first = s.m == m ? g : 256;
+    if (R <= 1) first = min(first, lane_xor<1>(first));
+    if (R <= 2) first = min(first, lane_xor<2>(first));
+    if (R <= 4) first = min(first, lane_xor<4>(first));
+    if (R <= 8) first = min(first, lane_xor<8>(first));
+    first = min(first, lane_xor<16>(first));
+    first = min(first, lane_xor<32>(first));
+    if (lane < R) sh[1][wave][lane] = (float)first;
+    __syncthreads();
+    return (int)fminf(fminf(sh[1][0][r], sh[1][1][r]), fminf(sh[1][2][r], sh[1][3][r])) == g;
+  };
+  const bool holds = holder();
+  Stat mine = s;
+  if (!holds) mine = stat_merge(Stat{m, 0.f, 0.f}, s, a.inv_t);  // (over: without the 1 that it then has too much)
+  __syncthreads();
+  const auto add = [](float x, float y) { return x + y; };
+  const float excess = over(mine.over, add, 1), s1 = over(mine.s1, add, 2);
   if (g == 0 && in) {
-    const float ls = logf(s.s0), l = m * a.inv_t + ls;
-    row_lse[r] = l;
-    a.lse[row] = l;
-    a.entropy[row] = ls - s.s1 / s.s0;
+    const float ls = log1pf(excess);
+    row_max[r] = m;
+    row_log[r] = ls;
+    a.lse[row] = m * a.inv_t + ls;
+    a.entropy[row] = ls - s1 / (1.f + excess);
     const int y = a.targets[row];
     a.logprob[row] = y >= 0 && y < a.V ? (a.ztgt[row] - m) * a.inv_t - ls : 0.f;
   }
@@ -374,8 +392,8 @@ __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
       int32_t* const ids = a.top_ids + (size_t)t * a.top;
       float* const lps = a.top_logprob + (size_t)t * a.top;
       bool done = false;
-      if (n <= 12) done = rank_logits<12>(row_logits, a.V, places, n, a.top, lane, keys, cols, a.inv_t, row_lse[q], ids, lps);
-      else if (n <= kQuickParts) done = rank_logits<kQuickParts>(row_logits, a.V, places, n, a.top, lane, keys, cols, a.inv_t, row_lse[q], ids, lps);
+      if (n <= 12) done = rank_logits<12>(row_logits, a.V, places, n, a.top, lane, keys, cols, a.inv_t, row_max[q], row_log[q], ids, lps);
+      else if (n <= kQuickParts) done = rank_logits<kQuickParts>(row_logits, a.V, places, n, a.top, lane, keys, cols, a.inv_t, row_max[q], row_log[q], ids, lps);
       PT_WAVE_LDS_FENCE();
       if (done) continue;
     }
@@ -395,11 +413,11 @@ __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
       cand[k * kPart + lane] = col < a.V ? order_key(a.logits[(size_t)t * a.ldl + col]) : 0u;
     }
     PT_WAVE_LDS_FENCE();
-    const float lse = row_lse[q];
+    const float m = row_max[q], ls = row_log[q];
     wave_select(cand, kp * kPart, a.top, lane, [&](int k, uint32_t key, uint32_t i) {
       if (lane == 0) {
         a.top_ids[(size_t)t * a.top + k] = sel[i >> 6] * kPart + (int)(i & 63);
-        a.top_logprob[(size_t)t * a.top + k] = order_value(key) * a.inv_t - lse;
+        a.top_logprob[(size_t)t * a.top + k] = (order_value(key) - m) * a.inv_t - ls;
       }
     });
     PT_WAVE_LDS_FENCE();
@@ -486,8 +504,8 @@ struct DzArgs {
 };
 
 template <typename T, typename S>
-__global__ void __launch_bounds__(64 * S::waves, 2) dz_kernel(DzArgs a) {
-  PT_SHARED(S)
+__global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) dz_kernel(DzArgs a) {
+  PT_LDS(S)
   constexpr int MT = S::MT;
   const int nb_m = (a.T + S::rows - 1) / S::rows;
   const int item = pt_item(nb_m * a.tiles_n);
@@ -496,7 +514,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) dz_kernel(DzArgs a) {
   pt_tile_pos(item, nb_m, a.tiles_n, tm, tn);
   tn += a.tile0;
   pt_f32x16 acc[2][MT];
-  pt_product<T, false, false, S>(a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, la0, lw0, la1, lw1, acc);
+  PT_PRODUCT(T, false, false, a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
@@ -526,7 +544,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) dz_kernel(DzArgs a) {
     }
   }
   const bool edge = a.V - col0 < 64 || row0 + 32 * MT > a.T;  // some of the wave's columns or rows do not exist: zeros
-  char* const ep = pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
+  char* const ep = PT_WAVE_LDS;
   T* const dz = (T*)a.dz + (size_t)row0 * a.ldz + col0;
   if constexpr (sizeof(T) == 2) {
     pt_hand_out<8, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, float(&v)[8], int) {
@@ -580,8 +598,8 @@ __device__ __forceinline__ void out_store(const OutArgs& a, int row, int col, pt
 }
 
 template <typename T, bool AK, bool WK, typename S>
-__global__ void __launch_bounds__(64 * S::waves, 2) out_kernel(OutArgs a) {
-  PT_SHARED(S)
+__global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) out_kernel(OutArgs a) {
+  PT_LDS(S)
   constexpr int MT = S::MT;
   // (rows are walked as columns are elsewhere: dW has many of them, dh is cut along K)
   const int nb_m = a.tiles_n, nb_n = (a.N + S::cols - 1) / S::cols;
@@ -592,13 +610,12 @@ __global__ void __launch_bounds__(64 * S::waves, 2) out_kernel(OutArgs a) {
   pt_tile_pos(item - z * nb_m * nb_n, nb_m, nb_n, tm, tn);
   tm += a.tile0;
   pt_f32x16 acc[2][MT];
-  pt_product<T, AK, WK, S>(a.A, a.lda, tm * S::rows, a.M, a.W, a.ldw, tn * S::cols, a.N, z * a.k_slice,
-                           min(a.K, (z + 1) * a.k_slice), la0, lw0, la1, lw1, acc);
+  PT_PRODUCT(T, AK, WK, a.A, a.lda, tm * S::rows, a.M, a.W, a.ldw, tn * S::cols, a.N, z * a.k_slice, min(a.K, (z + 1) * a.k_slice));
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
-  char* const ep = pt_wave_lds<S>(la0, lw0, la1, lw1, wave);
+  char* const ep = PT_WAVE_LDS;
   if (a.slices > 1) {
     float* const o = a.slab + (size_t)z * a.M * a.lds;
     pt_hand_out<4, MT>(ep, lane, acc, PtNothing(), [&](int r, int c, pt_f32x4 v, int) {

@@ -162,6 +162,46 @@ def test_one_sure_token_and_large_logits():
     assert (grad["d_hidden"] == 0).all() and (grad["d_weight"] == 0).all()
 
 
+@pytest.mark.parametrize("dtype,V,k", [("fp16", 50304, 2), ("bf16", 700, 0), ("fp32", 700, 3)])
+@pytest.mark.parametrize("T", [1, 300])
+def test_a_token_with_nearly_everything_keeps_its_bits(T, dtype, V, k):
+    """Row t's token is ahead by 4 + t % 12, so its log-probability is about -e^-16 at the least: held relative to itself, as is the
+    entropy.  Beside the bars above (of values, where x is at most the row's spread of logits) the two sums of the entropy are of one
+    sign, log1p adds 2^-22, and exp's argument, rounded three times, is off by 3 * 2^-24 x."""
+    import torch
+    g = np.random.default_rng(V + T)
+    w = np.clip(np.round(g.normal(0, 0.04, (V, 64)) * 1024), -127, 127) / 1024
+    w[:, 0] = 0
+    y = g.integers(0, V, T).astype(np.int32)
+    h = np.round(g.normal(0, 1, (T, 64)) * 16) / 16
+    w2 = np.zeros((V, 32))  # 32 more features: a token has its own sign pattern there, a row its token's, times what leads by enough
+    w2[:, :17] = 1 - 2.0 * ((np.arange(V)[:, None] >> np.arange(17)) & 1)
+    want = []
+    for t in range(T):
+        z = h[t] @ w.T
+        z0 = w2 @ w2[y[t]]  # 17, at others at most 15
+        want.append(np.ceil(max(0.0, (4 + t % 12 + np.delete(z, y[t]).max() - z[y[t]]) / 2) * 8) / 8)
+        assert (np.delete(z0, y[t]) <= 15).all()
+    h2 = np.array(want)[:, None] * w2[y]
+    h, w = np.concatenate([h, h2], 1), np.concatenate([w, w2], 1)
+    dev = [torch.from_numpy(x).to("cuda", _dt(dtype)) for x in (h, w)]
+    assert all((x.cpu().numpy() == e).all() for x, e in zip((dev[0].double(), dev[1].double()), (h, w)))
+    got = P.token_stats(dev[0], dev[1], torch.from_numpy(y).cuda(), 1.0, k)
+    z = h @ w.T
+    x = z - z[np.arange(T), y][:, None]
+    assert (np.sort(x, 1)[:, -2] <= -4).all()
+    rest = np.where(x < 0, np.exp(x), 0).sum(1)
+    lp = -np.log1p(rest)
+    ent = -lp - np.where(x < 0, np.exp(x) * x, 0).sum(1) / (1 + rest)
+    tol = 2.0**-22 * (2 + np.abs(x).max(1)) + 2.0**-21 + (100 + V / 64) * 2.0**-24
+    for name, value in (("logprobs", lp), ("entropy", ent)):
+        err = np.abs(got[name].cpu().numpy() - value) / np.abs(value)
+        assert (err <= 2 * tol).all(), (name, err.max())
+    if k:
+        assert (got["top_ids"][:, 0].cpu().numpy() == y).all()
+        assert (got["top_logprobs"][:, 0] == got["logprobs"]).all()
+
+
 def test_rows_that_are_not_numbers_stay_alone():
     import torch
     h, w, y, th, tw, ty = _inputs(9, 64, 500, "bf16", 3)
