@@ -277,7 +277,7 @@ __device__ __forceinline__ void store_symmetric(pt_f32x16 (&acc)[S::NT][S::MT], 
 // A = X X^T (the shorter side's), scaled
 template <typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_gram_kernel(const Group* __restrict__ g, int cur) {
-  PT_LDS(S)
+  PT_STAGES(S)
   int tile;
   const Prob& p = find_tile(g, kGram, tile);
   if (tile < 0) return;
@@ -287,16 +287,16 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_gram_kerne
   pt_f32x16 acc[S::NT][S::MT];
   const half_t* const x = p.xh[cur];
   if (p.m.rows > p.m.cols)
-    PT_PRODUCT(half_t, true, true, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp);
+    PT_PRODUCT(half_t, true, true, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.rp, nullptr);
   else
-    PT_PRODUCT(half_t, false, false, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld);
+    PT_PRODUCT(half_t, false, false, x, p.ld, tm * S::rows, p.sp, x, p.ld, tn * S::cols, p.sp, 0, p.ld, nullptr);
   store_symmetric<S, false>(acc, nullptr, p.a, p.sp, tm, tn, kAScale / (kXScale * kXScale), 0.f, PT_WAVE_LDS);
 }
 
 // B = b A + c A^2
 template <typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_poly_kernel(const Group* __restrict__ g) {
-  PT_LDS(S)
+  PT_STAGES(S)
   int tile;
   const Prob& p = find_tile(g, kPoly, tile);
   if (tile < 0) return;
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_poly_kerne
   pt_tile_triangle(tile, tm, tn);
   if (tm * S::rows >= p.sp) return;
   pt_f32x16 acc[S::NT][S::MT];
-  PT_PRODUCT(half_t, false, false, p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp);
+  PT_PRODUCT(half_t, false, false, p.a, p.sp, tm * S::rows, p.sp, p.a, p.sp, tn * S::cols, p.sp, 0, p.sp, nullptr);
   store_symmetric<S, true>(acc, p.a, p.b, p.sp, tm, tn, kC / kAScale, kB, PT_WAVE_LDS);
 }
 
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_poly_kerne
 template <typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_update_kernel(const Group* __restrict__ g, int cur, int last) {
   const MuonScalars c = g->c;
-  PT_LDS(S)
+  PT_STAGES(S)
   constexpr int MT = S::MT;
   int tile;
   const Prob& p = find_tile(g, kUpdate, tile);
@@ -322,9 +322,9 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) muon_update_ker
   pt_tile_pos(tile, nb_m, nb_n, tm, tn);
   pt_f32x16 acc[2][MT];
   if (p.m.rows > p.m.cols)
-    PT_PRODUCT(half_t, false, false, p.xh[cur], p.ld, tm * S::rows, p.rp, p.b, p.sp, tn * S::cols, p.sp, 0, p.sp);
+    PT_PRODUCT(half_t, false, false, p.xh[cur], p.ld, tm * S::rows, p.rp, p.b, p.sp, tn * S::cols, p.sp, 0, p.sp, nullptr);
   else
-    PT_PRODUCT(half_t, false, true, p.b, p.sp, tm * S::rows, p.sp, p.xh[cur], p.ld, tn * S::cols, p.ld, 0, p.sp);
+    PT_PRODUCT(half_t, false, true, p.b, p.sp, tm * S::rows, p.sp, p.xh[cur], p.ld, tn * S::cols, p.ld, 0, p.sp, nullptr);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

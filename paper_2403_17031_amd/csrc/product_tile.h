@@ -44,11 +44,19 @@ __device__ __forceinline__ pt_f32x16 pt_mma(float, pt_u32x4 w, pt_u32x4 a, pt_f3
 #define PT_GLOBAL(p) ((const __attribute__((address_space(1))) void*)(p))
 #define PT_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
-// WM x WN waves of MT x NT accumulators of 32 x 32; RING stages of LDS (2: see pt_product, more: pt_product_ring)
-template <int WM_, int WN_, int MT_, int NT_, int RING_ = 2>
+#define PT_WAVE_LDS_FENCE()                          \
+  __builtin_amdgcn_sched_barrier(0);                 \
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); \
+  __builtin_amdgcn_wave_barrier();                   \
+  __builtin_amdgcn_sched_barrier(0);
+
+// WM x WN waves of MT x NT accumulators of 32 x 32; RING stages of LDS (2: see pt_product, more: pt_product_ring); KW such sets of
+// waves, each with its quarter of every stage (4, or 1).
+template <int WM_, int WN_, int MT_, int NT_, int RING_ = 2, int KW_ = 1>
 struct PtShape {
-  static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, RING = RING_;
-  static constexpr int waves = WM * WN, rows = 32 * MT * WM, cols = 32 * NT * WN, stage = (rows + cols) * 128;
+  static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, RING = RING_, KW = KW_;
+  static constexpr int waves = WM * WN * KW, rows = 32 * MT * WM, cols = 32 * NT * WN, stage = (rows + cols) * 128;
+  static_assert(KW == 1 || (KW == 4 && RING > 2 && 3 * WM * WN * MT * NT * 4096 <= RING * stage), "quarters, their sums in the ring");
 };
 
 // One operand's tile loads: this lane's 16-byte chunks of a stage, as byte offsets from a uniform base.
@@ -57,6 +65,8 @@ struct PtLoads {
   static constexpr int E = 16 / (int)sizeof(T), KD = 128 / (int)sizeof(T), L = ROWS / (8 * NW);
   static constexpr int RB = KM ? ROWS * (int)sizeof(T) : 128;  // bytes of a stage's LDS row
   const char* base;
+  const char* end = nullptr;  // where the stage `at_end` lies instead
+  int at_end = -1;
   uint32_t off[L];
   size_t step;
 
@@ -65,9 +75,10 @@ struct PtLoads {
     const int r = lds_row(i, wave, lane), pos = ((1024 * (L * wave + i) + 16 * lane) % RB) / 16;
     return KM ? pos ^ (2 * (r & 3)) : pos ^ ((r >> 1) & 7);
   }
+  __device__ __forceinline__ const char* stage_at(int stage) const { return KM && stage == at_end ? end : base + stage * step; }
   // the same through load_to_lds, for a caller that counts its waits
   __device__ __forceinline__ void load_counted(uint32_t lds, int stage, int i, int wave) const {
-    load_to_lds(base + stage * step, off[i], lds + 1024 * (L * wave + i));
+    load_to_lds(stage_at(stage), off[i], lds + 1024 * (L * wave + i));
   }
   // the operand from its row r0 (of `extent`) on, from k0 on
   __device__ void init(const void* p, uint32_t ld, int r0, int extent, int k0, int wave, int lane) {
@@ -83,7 +94,7 @@ struct PtLoads {
     }
   }
   __device__ __forceinline__ void load(char* lds, int stage, int i, int wave) const {
-    const char* p = base + stage * step;
+    const char* p = stage_at(stage);
     asm volatile("" : "+s"(p));  // (uniform: a scalar base and the lane's 32-bit offset)
     uint32_t o = off[i];
     asm volatile("" : "+v"(o));
@@ -133,10 +144,11 @@ struct PtFrags {
 };
 
 // acc = the product over k0 <= k < k1 of one tile; la*, lw*: the stages' LDS (separate variables, so that a read of one stage does not
-// wait for the loads into the other).  k1 - k0 is a positive multiple of a stage's depth.
+// wait for the loads into the other).  k1 - k0 is a positive multiple of a stage's depth.  w_end: the last stage of a K-major W lies
+// there, with W's row stride, where W itself ends inside of it; or null.
 template <typename T, bool AK, bool WK, typename S>
 __device__ __forceinline__ void pt_product(const void* A, uint32_t lda, int m0, int M, const void* W, uint32_t ldw, int n0, int N,
-                                           int k0, int k1, char* la0, char* lw0, char* la1, char* lw1,
+                                           int k0, int k1, const void* w_end, char* la0, char* lw0, char* la1, char* lw1,
                                            pt_f32x16 (&acc)[S::NT][S::MT]) {
   constexpr int MT = S::MT, NT = S::NT, F = MT + NT, NMF = MT * NT;
   using LA = PtLoads<T, AK, S::rows, S::waves>;
@@ -156,6 +168,10 @@ __device__ __forceinline__ void pt_product(const void* A, uint32_t lda, int m0, 
 #pragma unroll
   for (int j = 0; j < NT; ++j) rw[j].init(wn + 32 * j, lane);
   const int nk = (k1 - k0) / LA::KD;
+  if (WK && w_end) {
+    gw.end = (const char*)w_end + (size_t)n0 * sizeof(T);
+    gw.at_end = nk - 1;
+  }
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -225,17 +241,19 @@ __device__ __forceinline__ void pt_product(const void* A, uint32_t lda, int m0, 
 
 // The same with a ring of S::RING stages, all but one of them under way while one is used: for launches whose tiles do not fill
 // the chip, where a stage's loads take longer than its multiplications.  The compiler does not know of the loads; what orders
-// them is the counted wait before the barrier.  Ends as pt_product does.
+// them is the counted wait before the barrier.  Ends as pt_product does; with quarters, the first set of waves has the sums
+// and the others are done (pt_done).
 template <typename T, bool AK, bool WK, typename S>
 __device__ __forceinline__ void pt_product_ring(const void* A, uint32_t lda, int m0, int M, const void* W, uint32_t ldw, int n0, int N,
-                                                int k0, int k1, char* lds, pt_f32x16 (&acc)[S::NT][S::MT]) {
+                                                int k0, int k1, const void* w_end, char* lds, pt_f32x16 (&acc)[S::NT][S::MT]) {
   constexpr int MT = S::MT, NT = S::NT, F = MT + NT, D = S::RING;
   using LA = PtLoads<T, AK, S::rows, S::waves>;
   using LW = PtLoads<T, WK, S::cols, S::waves>;
   constexpr int NL = LA::L + LW::L;
   static_assert((D - 1) * NL < 64, "the wait counts to 63");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = (wave / S::WN) * 32 * MT, wn = (wave % S::WN) * 32 * NT;
+  const int of = wave % (S::WM * S::WN), quarter = wave / (S::WM * S::WN);
+  const int wm = (of / S::WN) * 32 * MT, wn = (of % S::WN) * 32 * NT;
   LA ga;
   LW gw;
   ga.init(A, lda, m0, M, k0, wave, lane);
@@ -247,6 +265,10 @@ __device__ __forceinline__ void pt_product_ring(const void* A, uint32_t lda, int
 #pragma unroll
   for (int j = 0; j < NT; ++j) rw[j].init(wn + 32 * j, lane);
   const int nk = (k1 - k0) / LA::KD;
+  if (WK && w_end) {
+    gw.end = (const char*)w_end + (size_t)n0 * sizeof(T);
+    gw.at_end = nk - 1;
+  }
   const uint32_t lds_at = (uint32_t)(uintptr_t)PT_LDS(lds);
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -297,6 +319,44 @@ __device__ __forceinline__ void pt_product_ring(const void* A, uint32_t lda, int
   for (int u = 0; u < D - 1; ++u)
     if (u < nk) load_all(u, u);
   wait(min(D - 2, nk - 1));
+  if constexpr (S::KW > 1) {
+    frags(0, quarter, 0);
+    for (int kt = 0, slot = 0; kt < nk; ++kt) {
+      const int next = slot + 1 == D ? 0 : slot + 1, last = slot == 0 ? D - 1 : slot - 1;
+      if (kt + D - 1 < nk) load_all(last, kt + D - 1);
+      wait(max(0, min(D - 2, nk - 2 - kt)));
+      frags(next, quarter, 1);
+      mul(0);
+#pragma unroll
+      for (int n = 0; n < MT; ++n) fa[0][n] = fa[1][n];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) fw[0][n] = fw[1][n];
+      slot = next;
+    }
+    // (the others' sums, in the order of the quarters)
+    auto each = [&](int q, auto f) {
+      char* const at = lds + ((q - 1) * S::WM * S::WN + of) * MT * NT * 4096 + lane * 16;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) f(acc[j][i], 4 * x, (pt_f32x4*)(at + ((j * MT + i) * 4 + x) * 1024));
+    };
+    if (quarter)
+      each(quarter, [](pt_f32x16& c, int e, pt_f32x4* to) { *to = pt_f32x4{c[e], c[e + 1], c[e + 2], c[e + 3]}; });
+    __syncthreads();
+    if (quarter) return;
+#pragma unroll
+    for (int q = 1; q < S::KW; ++q)
+      each(q, [](pt_f32x16& c, int e, pt_f32x4* from) {
+        const pt_f32x4 v = *from;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) c[e + u] += v[u];
+      });
+    PT_WAVE_LDS_FENCE();
+    return;
+  }
   frags(0, 0, 0);
   for (int kt = 0, slot = 0; kt < nk; ++kt) {
     const int next = slot + 1 == D ? 0 : slot + 1, last = slot == 0 ? D - 1 : slot - 1;
@@ -319,12 +379,6 @@ __device__ __forceinline__ void pt_product_ring(const void* A, uint32_t lda, int
 // The accumulators of a wave: element e of acc[j][i] is row 32 i + lane % 32, column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4.
 __device__ __forceinline__ int pt_col(int j, int e, int hf) { return 32 * j + 8 * (e >> 2) + 4 * hf + (e & 3); }
 
-#define PT_WAVE_LDS_FENCE()                          \
-  __builtin_amdgcn_sched_barrier(0);                 \
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); \
-  __builtin_amdgcn_wave_barrier();                   \
-  __builtin_amdgcn_sched_barrier(0);
-
 // After the product a wave has 16 KB of it to itself: every wave has passed the last barrier with all that it read of the stages.
 template <typename S>
 __device__ __forceinline__ char* pt_wave_lds(char* la0, char* lw0, char* la1, char* lw1, int wave) {
@@ -342,7 +396,7 @@ __device__ __forceinline__ char* pt_any_wave_lds(char* ring, char* la0, char* lw
 }
 
 // One tile's product into acc, whichever way the shape keeps its stages (a ring's are one array), and the LDS a wave has afterwards.
-#define PT_LDS(S)                                                                     \
+#define PT_STAGES(S)                                                                   \
   constexpr bool kRing = S::RING > 2;                                                 \
   __shared__ __attribute__((aligned(16))) char ring[kRing ? S::RING * S::stage : 16]; \
   __shared__ __attribute__((aligned(16))) char la0[kRing ? 16 : S::rows * 128];       \
@@ -358,8 +412,13 @@ __device__ __forceinline__ char* pt_any_wave_lds(char* ring, char* la0, char* lw
 using PtBig = PtShape<2, 4, 4, 2>;       // 256 x 256, 8 waves of 128 x 64, a CU to itself
 using PtMid = PtShape<2, 2, 2, 2>;       // 128 x 128, 4 waves of 64 x 64, two blocks on a CU
 using PtSmall = PtShape<2, 1, 1, 2, 4>;  // 64 x 64, 2 waves of 32 x 64, a ring of four stages, two blocks on a CU
+using PtThin = PtShape<1, 1, 1, 2, 4, 4>;  // 32 x 64, 4 waves that each take a quarter of every stage, three blocks on a CU
 template <typename S>
-constexpr int pt_waves_eu = S::RING > 2 ? 1 : 2;  // for __launch_bounds__
+constexpr int pt_waves_eu = S::KW > 1 ? 3 : S::RING > 2 ? 1 : 2;  // for __launch_bounds__
+template <typename S>
+__device__ __forceinline__ bool pt_done(int wave) {  // after a product: this wave's results are another's
+  return S::KW > 1 && wave >= S::WM * S::WN;
+}
 
 // Hands a wave's results out in memory order: 64 rows of its 64 columns at a time pass through its LDS as float (16-byte chunks XORed with
 // the row), since a store from the accumulators would touch 32 rows with 16 bytes each.  sink(row, col, v, it): N (4 or 8)

@@ -49,7 +49,7 @@ struct StatsArgs {
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) stats_kernel(StatsArgs a) {
-  PT_LDS(S)
+  PT_STAGES(S)
   constexpr int MT = S::MT;
   const int nb_m = (a.T + S::rows - 1) / S::rows;
   const int item = pt_item(nb_m * a.tiles_n);
@@ -58,10 +58,11 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) stats_kernel(St
   pt_tile_pos(item, nb_m, a.tiles_n, tm, tn);
   tn += a.tile0;
   pt_f32x16 acc[2][MT];
-  PT_PRODUCT(T, false, false, a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d);
+  PT_PRODUCT(T, false, false, a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, nullptr);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
+  if (pt_done<S>(wave)) return;
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
   if (col0 >= a.V) return;
   const int part = col0 / kPart;
@@ -505,7 +506,7 @@ struct DzArgs {
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) dz_kernel(DzArgs a) {
-  PT_LDS(S)
+  PT_STAGES(S)
   constexpr int MT = S::MT;
   const int nb_m = (a.T + S::rows - 1) / S::rows;
   const int item = pt_item(nb_m * a.tiles_n);
@@ -514,10 +515,11 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) dz_kernel(DzArg
   pt_tile_pos(item, nb_m, a.tiles_n, tm, tn);
   tn += a.tile0;
   pt_f32x16 acc[2][MT];
-  PT_PRODUCT(T, false, false, a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d);
+  PT_PRODUCT(T, false, false, a.h, a.ldh, tm * S::rows, a.T, a.w, a.ldw, tn * S::cols, a.V, 0, a.d, nullptr);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hf = lane >> 5;
+  if (pt_done<S>(wave)) return;
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
   if (row0 >= a.rows || col0 >= a.ldz) return;
   const float s = (a.scale ? a.scale[0] : 1.f) * a.inv_t;
@@ -567,7 +569,7 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) dz_kernel(DzArg
 
 // out [M, N] (T or float) = scale * A W', or the fp32 slabs of a product cut along K
 struct OutArgs {
-  const void *A, *W;
+  const void *A, *W, *w_end;  // (see pt_product)
   uint32_t lda, ldw;
   int M, N, K, slices, k_slice;
   const float* scale;  // null: 1
@@ -599,7 +601,7 @@ __device__ __forceinline__ void out_store(const OutArgs& a, int row, int col, pt
 
 template <typename T, bool AK, bool WK, typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) out_kernel(OutArgs a) {
-  PT_LDS(S)
+  PT_STAGES(S)
   constexpr int MT = S::MT;
   // (rows are walked as columns are elsewhere: dW has many of them, dh is cut along K)
   const int nb_m = a.tiles_n, nb_n = (a.N + S::cols - 1) / S::cols;
@@ -610,10 +612,12 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) out_kernel(OutA
   pt_tile_pos(item - z * nb_m * nb_n, nb_m, nb_n, tm, tn);
   tm += a.tile0;
   pt_f32x16 acc[2][MT];
-  PT_PRODUCT(T, AK, WK, a.A, a.lda, tm * S::rows, a.M, a.W, a.ldw, tn * S::cols, a.N, z * a.k_slice, min(a.K, (z + 1) * a.k_slice));
+  const int k1 = min(a.K, (z + 1) * a.k_slice);
+  PT_PRODUCT(T, AK, WK, a.A, a.lda, tm * S::rows, a.M, a.W, a.ldw, tn * S::cols, a.N, z * a.k_slice, k1, k1 == a.K ? a.w_end : nullptr);
   int lane = threadIdx.x & 63;
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (pt_done<S>(wave)) return;
   const int row0 = tm * S::rows + wave / S::WN * 32 * MT, col0 = tn * S::cols + wave % S::WN * 64;
   char* const ep = PT_WAVE_LDS;
   if (a.slices > 1) {
@@ -680,11 +684,16 @@ __global__ void __launch_bounds__(256) narrow_rows_kernel(const float* __restric
 
 int tiles(int m, int n, int tm, int tn) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); }
 
+size_t elem_size(int dtype) { return dtype == kTokensF32 ? 4 : 2; }
+int stage_of(int dtype) { return 128 / (int)elem_size(dtype); }  // k of a stage of the products
+int whole(int n, int stage) { return (n + stage - 1) / stage * stage; }
+int padded(int n) { return whole(n, 64); }
+
 // How a product's columns are cut: `big` column tiles of 256 (256 x 256, a CU each) first, the rest in tiles of 128 (128 x 128, two
 // on a CU).  16-bit types: a round of 256 large tiles takes 1.95 us a stage, one of 512 small ones 1.5 (and of up to 256 1.0), so
 // the large ones make whole rounds and the small ones what is left.  float: the matrix instructions take 16 times as long and
 // nothing else counts: per tile as much as its area.
-int big_columns(int M, int N, int dtype) {
+int big_columns(int M, int N, int dtype, double* takes = nullptr) {
   const int nb_m = (M + 255) / 256, nb_n = (N + 255) / 256, mid_m = (M + 127) / 128, mid_n = (N + 127) / 128;
   const double round = dtype == kTokensF32 ? 4.0 : 1.95, small = dtype == kTokensF32 ? 2.0 : 1.5, half = dtype == kTokensF32 ? 1.05 : 1.0;
   auto cost = [&](int n) {
@@ -696,7 +705,17 @@ int big_columns(int M, int N, int dtype) {
   double best_c = cost(0);
   for (int n = nb_n; n > 0; --n)
     if (cost(n) < best_c - 1e-9) best = n, best_c = cost(n);
+  if (takes) *takes = best_c;
   return best;
+}
+// Or 32 x 64, whose four waves share a tile's K: for few rows, whose tiles would be mostly empty, and for few tiles.
+constexpr double kThinStart = 6;  // stages that a tile's start and end take
+double thin_cost(int n, int dtype) { return dtype == kTokensF32 ? 0.15 * ((n + 255) / 256) : 1e9; }
+bool thin(int M, int N, int K, int dtype) {
+  double wide;
+  big_columns(M, N, dtype, &wide);
+  const int stages = (K + stage_of(dtype) - 1) / stage_of(dtype);
+  return thin_cost(tiles(M, N, 32, 64), dtype) * (stages + kThinStart) < wide * (stages + 1.5);
 }
 
 struct Bump {
@@ -710,11 +729,6 @@ struct Bump {
     return p;
   }
 };
-
-size_t elem_size(int dtype) { return dtype == kTokensF32 ? 4 : 2; }
-int stage_of(int dtype) { return 128 / (int)elem_size(dtype); }  // k of a stage of the products
-int whole(int n, int stage) { return (n + stage - 1) / stage * stage; }
-int padded(int n) { return whole(n, 64); }
 
 constexpr int kLogitRows = 16384;  // rows of stored logits at a time
 constexpr int kGradRows = 16384;   // rows of dz at a time
@@ -732,22 +746,26 @@ void by_type(int dtype, F f) {
 }
 
 struct Operand {
-  const void* p;
+  const void *p, *end;  // end: the last rows, up to a whole stage of them, where they are summed over and are not one
   uint32_t ld;
 };
-// The matrix as the products read it: as it lies, or a copy in the workspace with zeros up to whole stages (p null: measuring).
-Operand packed(Bump& ws, const TokenRows& m, int rows, int d, int dtype, hipStream_t s) {
-  if (m.lies_well) return {m.p, (uint32_t)m.ld};
-  const int ldd = padded(d), rows_to = padded(rows);
-  char* const to = ws.take<char>((size_t)rows_to * ldd * elem_size(dtype));
-  if (to)
-    by_type(dtype, [&](auto t) {
-      using T = decltype(t);
-      const size_t chunks = (size_t)rows_to * ldd / (16 / sizeof(T));
-      hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const T*)m.p, (size_t)m.ld, rows, d,
-                         (T*)to, ldd, rows_to);
-    });
-  return {to, (uint32_t)ldd};
+// The matrix as the products read it: as it lies, or a copy in the workspace with zeros up to whole stages (a null workspace: measuring).
+// Where its rows are summed over and it ends inside a stage, that stage alone is copied.
+Operand packed(Bump& ws, const TokenRows& m, int rows, int d, int dtype, bool rows_as_k, hipStream_t s) {
+  auto copy = [&](int from, int n, int ldd, int rows_to) {
+    char* const to = ws.take<char>((size_t)rows_to * ldd * elem_size(dtype));
+    if (to)
+      by_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        const size_t chunks = (size_t)rows_to * ldd / (16 / sizeof(T));
+        hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const T*)m.p + (size_t)from * m.ld,
+                           (size_t)m.ld, n, d, (T*)to, ldd, rows_to);
+      });
+    return to;
+  };
+  if (!m.lies_well) return {copy(0, rows, padded(d), padded(rows)), nullptr, (uint32_t)padded(d)};
+  const int stage = stage_of(dtype), over = rows % stage;
+  return {m.p, rows_as_k && over ? copy(rows - over, over, (int)m.ld, stage) : nullptr, (uint32_t)m.ld};
 }
 
 size_t finish_lds(int parts, int rows, int top) {
@@ -772,13 +790,13 @@ int sample_tiles(int T, int V, int top) {
 }  // namespace
 
 bool token_rows_lie_well(int64_t ld, int d, int dtype, int rows_as_k) {
-  return ld % (16 / (int)elem_size(dtype)) == 0 && d % stage_of(dtype) == 0 && rows_as_k % stage_of(dtype) == 0;
+  return ld % (16 / (int)elem_size(dtype)) == 0 && d % stage_of(dtype) == 0 && (rows_as_k % stage_of(dtype) == 0 || ld <= 1 << 16);
 }
 
 size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s, hipError_t* err) {
   Bump ws{(char*)workspace};
   const int parts = (a.V + kPart - 1) / kPart;
-  const Operand h = packed(ws, a.hidden, a.T, a.d, a.dtype, s), w = packed(ws, a.weight, a.V, a.d, a.dtype, s);
+  const Operand h = packed(ws, a.hidden, a.T, a.d, a.dtype, false, s), w = packed(ws, a.weight, a.V, a.d, a.dtype, false, s);
   const int rows = a.top ? equal_chunk(a.T, kLogitRows) : a.T;
   StatsArgs k;
   float* const part = ws.take<float>((size_t)3 * parts * rows);
@@ -820,8 +838,12 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
         k.thr = thr;
         run(PtBig(), first, (a.V + 255) / 256);
       } else {
-        if (big) run(PtBig(), 0, big);
-        if (2 * big < mids) run(PtMid(), 2 * big, mids);
+        if (thin(n, a.V, a.d, a.dtype)) {
+          run(PtThin(), 0, parts);
+        } else {
+          if (big) run(PtBig(), 0, big);
+          if (2 * big < mids) run(PtMid(), 2 * big, mids);
+        }
       }
     });
     FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, a.inv_t,
@@ -844,26 +866,26 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
 // are cut along it: as many slices as make rounds times a slice's length shortest, each at least 512 long, with what the fp32
 // slabs cost to write and to read again (5 TB/s).
 struct OutPlan {
-  int slices, k_slice, big;
+  int slices, k_slice, big, thin;
 };
 static OutPlan out_plan(int M, int N, int K, int dtype) {
   const int stage = stage_of(dtype);
-  OutPlan best = {1, K, 0};
+  OutPlan best = {1, K, 0, 0};
   double best_t = 1e30;
   for (int z = 1; z <= 64; ++z) {
     const int q = whole((K + z - 1) / z, stage);
     if (z > 1 && (q < 512 || (K + q - 1) / q != z)) continue;
-    const double us = dtype == kTokensF32 ? 8.0 : 1.0;  // of a stage, in big_columns' units
+    const double us = dtype == kTokensF32 ? 2.0 : 1.0;  // of a stage, in big_columns' units
     const double slabs = z > 1 ? z * ((double)M * N * 8 / 5e6) + 4 : 0;
-    for (int big = 0; big < 2; ++big) {
-      const int n = big ? tiles(M, N, 256, 256) * z : tiles(M, N, 128, 128) * z;
-      const double rounds = big ? std::ceil(n / 256.0) * (dtype == kTokensF32 ? 4.0 : 1.95)
+    for (int big = 0; big < 3; ++big) {
+      const int n = big == 2 ? tiles(M, N, 32, 64) * z : big ? tiles(M, N, 256, 256) * z : tiles(M, N, 128, 128) * z;
+      const double rounds = big == 2 ? thin_cost(n, dtype) : big ? std::ceil(n / 256.0) * (dtype == kTokensF32 ? 4.0 : 1.95)
                                 : n / 512 * (dtype == kTokensF32 ? 2.0 : 1.5) + (n % 512 == 0 ? 0.0 : n % 512 <= 256 ? 1.0 : dtype == kTokensF32 ? 2.0 : 1.5);
-      const double t = rounds * us * (q / stage + 3) + slabs;
-      if (t < best_t) best_t = t, best = {z, q, big ? (M + 255) / 256 : 0};
+      const double t = rounds * us * (q / stage + (big == 2 ? kThinStart : dtype == kTokensF32 ? 1.5 : 3.0)) + slabs;
+      if (t < best_t) best_t = t, best = {z, q, big == 1 ? (M + 255) / 256 : 0, big == 2};
     }
   }
-  if (best.slices == 1) best.big = big_columns(N, M, dtype);
+  if (best.slices == 1 && !best.thin) best.big = big_columns(N, M, dtype);
   return best;
 }
 
@@ -877,8 +899,11 @@ static void launch_out(OutArgs& o, const OutPlan& p, hipStream_t s) {
     hipLaunchKernelGGL((out_kernel<T, AK, WK, S>), dim3(pt_grid(n)), dim3(64 * S::waves), 0, s, o);
   };
   const int mids = (o.M + 127) / 128;
+  if constexpr (sizeof(T) == 4) {
+    if (p.thin) run(PtThin(), 0, (o.M + 31) / 32);
+  }
   if (p.big) run(PtBig(), 0, p.big);
-  if (2 * p.big < mids) run(PtMid(), 2 * p.big, mids);
+  if (!p.thin && 2 * p.big < mids) run(PtMid(), 2 * p.big, mids);
   if (o.slices > 1) {
     const size_t n = (size_t)o.M * (o.lds / 4);
     hipLaunchKernelGGL(out_sum_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, o);
@@ -887,7 +912,7 @@ static void launch_out(OutArgs& o, const OutPlan& p, hipStream_t s) {
 
 size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStream_t s, hipError_t* err) {
   Bump ws{(char*)workspace};
-  const Operand h = packed(ws, a.hidden, a.T, a.d, a.dtype, s), w = packed(ws, a.weight, a.V, a.d, a.dtype, s);
+  const Operand h = packed(ws, a.hidden, a.T, a.d, a.dtype, true, s), w = packed(ws, a.weight, a.V, a.d, a.dtype, true, s);
   const int esz = (int)elem_size(a.dtype), stage = stage_of(a.dtype), rows = equal_chunk(a.T, kGradRows);
   const int ldz = padded(a.V), kv = whole(a.V, stage), lds = (a.d + 3) & ~3;
   const bool chunks = rows < a.T;
@@ -917,6 +942,7 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
     oh.lda = ldz;
     oh.W = w.p;
     oh.ldw = w.ld;
+    oh.w_end = w.end;
     oh.M = n;
     oh.N = a.d;
     oh.K = kv;
@@ -930,6 +956,7 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
     ow.lda = ldz;
     ow.W = hp;
     ow.ldw = h.ld;
+    ow.w_end = n % stage ? h.end : nullptr;  // (the last rows')
     ow.M = a.V;
     ow.N = a.d;
     ow.K = whole(n, stage);
@@ -952,8 +979,12 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
         hipLaunchKernelGGL((dz_kernel<T, S>), dim3(pt_grid(((n + S::rows - 1) / S::rows) * (to - from))), dim3(64 * S::waves), 0, s, k);
       };
       const int big = big_columns(n, a.V, a.dtype), mids = (a.V + 127) / 128;
-      if (big) run(PtBig(), 0, big);
-      if (2 * big < mids) run(PtMid(), 2 * big, mids);
+      bool done = false;
+      if constexpr (sizeof(T) == 4) {
+        if ((done = thin(n, a.V, a.d, a.dtype))) run(PtThin(), 0, ldz / 64);
+      }
+      if (!done && big) run(PtBig(), 0, big);
+      if (!done && 2 * big < mids) run(PtMid(), 2 * big, mids);
       launch_out<T, false, true>(oh, ph, s);
       launch_out<T, true, true>(ow, pw, s);
     });

@@ -253,6 +253,8 @@ GRADS = [  # T, d, V, type, type of the gradients
     (1, 64, 100, "bf16", "bf16"), (1, 1, 1, "fp32", "fp32"), (3, 37, 77, "fp16", "fp16"), (6, 64, 64, "fp32", "fp32"),
     (70, 128, 513, "bf16", "bf16"), (129, 96, 1000, "fp32", "fp32"), (257, 192, 640, "fp16", "fp32"), (300, 72, 2050, "fp16", "fp16"),
     (1000, 64, 3001, "bf16", "fp32"), (64, 1030, 130, "bf16", "bf16"), (2100, 640, 4200, "bf16", "bf16"),
+    (1, 64, 20011, "fp16", "fp16"), (33, 512, 40001, "bf16", "bf16"), (2, 128, 9999, "fp32", "fp32"), (40, 2048, 333, "fp32", "fp32"),
+    (95, 160, 6001, "fp32", "fp32"),
 ]
 
 
