@@ -30,7 +30,7 @@ namespace {
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kXScale = 2048.f, kAScale = 4096.f;
 constexpr int kProbs = kMuonGroup;  // of a launch
-constexpr int kNormElems = 16384;  // elements of a block of the norm
+constexpr int kNormElems = 4096;  // elements of a block of the norm
 constexpr size_t kGroupElems = (size_t)1 << 28;
 
 struct Prob {
@@ -145,7 +145,7 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return v;
 }
 
-// The momentum's update, and the sum of squares of 16,384 elements.
+// The momentum's update, and the sum of squares of 4,096 elements.
 __global__ void __launch_bounds__(256) muon_norm_kernel(const Group* __restrict__ g) {
   const MuonScalars c = g->c;
   __shared__ double sh[4];

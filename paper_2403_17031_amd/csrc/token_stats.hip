@@ -703,8 +703,10 @@ int big_columns(int M, int N, int dtype, double* takes = nullptr) {
   };
   int best = 0;
   double best_c = cost(0);
-  for (int n = nb_n; n > 0; --n)
-    if (cost(n) < best_c - 1e-9) best = n, best_c = cost(n);
+  for (int r = (nb_m * nb_n + 255) / 256; r > 0; --r) {  // (the most that r rounds hold)
+    const int n = std::min(nb_n, 256 * r / nb_m);
+    if (n > 0 && cost(n) < best_c - 1e-9) best = n, best_c = cost(n);
+  }
   if (takes) *takes = best_c;
   return best;
 }
@@ -772,17 +774,25 @@ size_t finish_lds(int parts, int rows, int top) {
   return top ? ((size_t)rows * (parts | 1) + (size_t)std::min(rows, 4) * finish_words(top)) * 4 : 0;
 }
 
-// Column tiles whose logits are stored whole, so that their part maxima bound what the others need to store: an eighth of the
-// vocabulary or so, a count that leaves both launches rounds of 256 tiles as full as any does; 0: one launch that stores all.  (13,568
-// rows of 50,304 entries, eight alternatives: all stored 3.33 ms, this way 3.0, no alternatives 2.74.)
-int sample_tiles(int T, int V, int top) {
-  const int nb_m = (T + 255) / 256, nb_n = (V + 255) / 256;
-  if (!top || nb_m * nb_n < 2048 || nb_n < 32) return 0;
-  int best = 0, best_r = INT_MAX;
-  for (int n = nb_n / 6; n >= nb_n / 12; --n) {
-    if (4 * n < 4 * top) break;
-    const int r = (nb_m * n + 255) / 256 + (nb_m * (nb_n - n) + 255) / 256;
-    if (r < best_r) best = n, best_r = r;
+// Column tiles of 256 whose logits are stored whole, so that their part maxima bound what the others need to store; 0: one launch
+// that stores all.  The shortest of rounds of tiles (see big_columns) times K's stages, what is stored at 5 TB/s (parts by
+// themselves at half of it), and 7 us for the bound and its launch.  (13,568 rows of 50,304 entries, K = 2,560, eight alternatives:
+// all stored 3.33 ms, this way 2.89, no alternatives 2.74; 1,003 rows of 50,277, K = 1,037, five: 203 and 196 us; 2,000 of 50,304,
+// K = 768, eight: 269 and 234.)
+int sample_tiles(int T, int V, int K, int top, int dtype) {
+  const int nb_n = (V + 255) / 256;
+  double all;
+  if (!top || !big_columns(T, V, dtype, &all)) return 0;
+  const double stage = (dtype == kTokensF32 ? 2.0 : 1.0) * ((K + stage_of(dtype) - 1) / stage_of(dtype) + 4), column = 256.0 * T * 4 / 5e6;
+  int best = 0;
+  double best_t = all * stage + nb_n * column;
+  for (int n = top; n <= std::min(nb_n / 2, 239); ++n) {  // (stats_threshold_kernel holds 16 rows of 4 n maxima in 60 KB)
+    double rest;
+    big_columns(T, V - 256 * n, dtype, &rest);
+    const double rounds = (((T + 255) / 256) * n + 255) / 256 * (dtype == kTokensF32 ? 4.0 : 1.95);
+    const double kept = (nb_n - n) * column * std::min(1.0, top / (4.0 * n));  // parts that the bound does not rule out
+    const double t = (rounds + rest) * stage + n * column + 2 * kept + 7;
+    if (t < best_t) best = n, best_t = t;
   }
   return best;
 }
@@ -831,12 +841,14 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
         hipLaunchKernelGGL((stats_kernel<T, S>), dim3(pt_grid(((n + S::rows - 1) / S::rows) * (to - from))), dim3(64 * S::waves), 0, s, k);
       };
       const int big = big_columns(n, a.V, a.dtype), mids = (a.V + 127) / 128;
-      if (const int first = sample_tiles(n, a.V, a.top)) {
+      if (const int first = sample_tiles(n, a.V, a.d, a.top, a.dtype)) {
         run(PtBig(), 0, first);
         hipLaunchKernelGGL(stats_threshold_kernel, dim3((n + 15) / 16), dim3(256), 16 * (size_t)(4 * first | 1) * 4, s, k.pmax, n, 4 * first,
                            a.top, thr);
         k.thr = thr;
-        run(PtBig(), first, (a.V + 255) / 256);
+        const int then = first + big_columns(n, a.V - 256 * first, a.dtype);
+        if (then > first) run(PtBig(), first, then);
+        if (2 * then < mids) run(PtMid(), 2 * then, mids);
       } else {
         if (thin(n, a.V, a.d, a.dtype)) {
           run(PtThin(), 0, parts);
