@@ -850,12 +850,12 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
         if (then > first) run(PtBig(), first, then);
         if (2 * then < mids) run(PtMid(), 2 * then, mids);
       } else {
-        if (thin(n, a.V, a.d, a.dtype)) {
-          run(PtThin(), 0, parts);
-        } else {
-          if (big) run(PtBig(), 0, big);
-          if (2 * big < mids) run(PtMid(), 2 * big, mids);
+        bool done = false;
+        if constexpr (sizeof(T) == 4) {
+          if ((done = thin(n, a.V, a.d, a.dtype))) run(PtThin(), 0, parts);
         }
+        if (!done && big) run(PtBig(), 0, big);
+        if (!done && 2 * big < mids) run(PtMid(), 2 * big, mids);
       }
     });
     FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, a.inv_t,
