@@ -964,8 +964,8 @@ int rlhf_token_stats(const void* hidden, int64_t ld_hidden, const void* weight, 
   if (!hidden || !weight || !targets || !out_logprobs || !out_entropy || !out_lse || !workspace)
     return fail(RLHF_EINVAL, "null pointer argument");
   if (top_k > 0 && (!out_top_ids || !out_top_logprobs)) return fail(RLHF_EINVAL, "top_k > 0 needs both of its outputs");
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-    return fail(RLHF_EINVAL, "temperature and its reciprocal must be finite and > 0");
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(2.0f / temperature))
+    return fail(RLHF_EINVAL, "temperature and twice its reciprocal must be finite and > 0");
   if ((((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)workspace) & 15) != 0)
     return fail(RLHF_EINVAL, "matrices and workspace must be 16-byte aligned");
   if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_token_stats_workspace_bytes reports");
@@ -1017,8 +1017,8 @@ int rlhf_token_stats_backward(const void* hidden, int64_t ld_hidden, const void*
   if (const int rc = rlhf_token_stats_backward_workspace_bytes(T, d, V, ld_hidden, ld_weight, dtype, grad_dtype, &need)) return rc;
   if (!hidden || !weight || !targets || !lse || !d_logprobs || !d_hidden || !d_weight || !workspace || (d_entropy && !entropy))
     return fail(RLHF_EINVAL, "null pointer argument");
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-    return fail(RLHF_EINVAL, "temperature and its reciprocal must be finite and > 0");
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(2.0f / temperature))
+    return fail(RLHF_EINVAL, "temperature and twice its reciprocal must be finite and > 0");
   if ((((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)workspace) & 15) != 0)
     return fail(RLHF_EINVAL, "matrices and workspace must be 16-byte aligned");
   if (workspace_bytes < need) return fail(RLHF_ENOMEM, "workspace smaller than rlhf_token_stats_backward_workspace_bytes reports");

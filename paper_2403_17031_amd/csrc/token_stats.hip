@@ -5,14 +5,20 @@
 //   dz_v = (g ([v = y] - p_v) - e p_v (log p_v + entropy)) / temperature,  dh = dz W,  dW = dz^T h.
 //
 // Forward: the product's epilogue leaves (max, S0, S1) of every part (the 64 columns of a wave) of a row, so without alternatives
-// no logit is stored.  With them the logits are stored, 4096 rows at a time, and read again at few places: an entry
-// among a row's k largest lies in one of the k parts whose maxima are largest (ties: the lower part, as the lower id among
-// equals), since each part before its own in that order holds an entry before it.  The second kernel picks those parts, then the
-// k entries among their 64 k logits.
+// no logit is stored.  With them: an entry among a row's k largest lies in one of the k parts whose maxima are largest (ties:
+// the lower part, as the lower id among equals), since each part before its own in that order holds an entry before it.  So the
+// first column tiles store their logits, which bounds the k-th largest maximum of each row, and the others store the
+// parts that reach the bound, 16,384 rows at a time (few rows: all is stored).  The last kernel merges the parts' sums, picks
+// those parts, then the k entries among their 64 k logits.
 //
-// Backward: the first product's epilogue forms dz (rounded to the operands' type: products of 16-bit operands are what the
-// matrix cores run at full rate, and the rounding, half a step of 2^-8 or 2^-11 relative, is that of the results in the same
-// type); dh and dW read it row-major and K-major, W and h as they lie.
+// Backward: the first product's epilogue forms dz, rounded to the operands' type: products of 16-bit operands are what the
+// matrix cores run at full rate (float is a tenth), and the rounding, half a step of 2^-8 or 2^-11 relative, is that of the results
+// in the same type.  Both roundings together: d_hidden is off by 0.23 % (bfloat16, 13,568 rows of a 2.8B model's width; 0.17 % if it
+// were only rounded at the end).  dh and dW read dz row-major and K-major, W and h as they lie.
+//
+// What bounds it: few rows read W (1 row, 50,304 x 2,560 in bfloat16: 62 us, 4.2 TB/s with the finishing kernel and the launches; a copy
+// reaches 5.0); many are matrix products (13,568 rows: 2.74 ms without alternatives, 1,275 TFLOP/s of the 1,290 that a
+// library product of this size reaches here; the gradient 8.75 ms, 1,200).
 #include <algorithm>
 #include <cmath>
 
@@ -47,6 +53,9 @@ struct StatsArgs {
   const float* thr;         // [T] or null: only parts whose maximum is not below their row's are stored
 };
 
+// A tile of logits in the accumulators and what is kept of it.  The epilogue is vector work (a maximum, an exponential and five more
+// instructions an entry) that the matrix cores wait for: 10 us of a tile of 256 x 256, whose product takes 1.7 us a stage, which is
+// why K = 768 runs at 60 % of the rate that K = 2,560 does.  13,568 x 50,304, K = 2,560: 2.6 ms of the call's 2.74.
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) stats_kernel(StatsArgs a) {
   PT_STAGES(S)
@@ -313,7 +322,8 @@ __device__ __forceinline__ int bounded_places(const uint32_t* keys, int n, int k
   return found;
 }
 
-// Block: R rows, 256 / R threads to each for the sums; then a wave per row for the alternatives.
+// Block: R rows, 256 / R threads to each for the sums; then a wave per row for the alternatives.  Bound by the latency of its few
+// dependent reads: 13,568 rows of 786 parts with eight alternatives 120 us (the parts' 128 MB would take 26), 1,003 rows 18, one row 9.
 // LDS: the keys of the rows' part maxima [R][parts | 1] (with alternatives), then of each wave its candidates' [top * 64] and the
 // parts [top], as chosen and by id, or (the quick way) the parts [32] and the keys and ids of what is ranked [64].
 template <int R>
@@ -426,6 +436,7 @@ __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
 }
 
 // thr[row] = a bound that `top` of the row's first `parts` maxima reach: no part below it can hold one of the row's top entries.
+// (13,568 rows, 112 parts: 15 us.)
 __global__ void __launch_bounds__(256) stats_threshold_kernel(const float* __restrict__ pmax, int T, int parts, int top, float* __restrict__ thr) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = parts | 1;
@@ -446,7 +457,7 @@ __global__ void __launch_bounds__(256) stats_threshold_kernel(const float* __res
 }
 
 // dst [rows_to][ldd] = src [rows][cols] (row stride lds), zero beyond either; 16 bytes of dst a thread.  Rows of src may start at
-// any element: its loads need no more alignment than that.
+// any element: its loads need no more alignment than that.  (50,277 x 1,037 halves: 37 us, 5.8 TB/s, some of it from the last cache.)
 template <typename T>
 __global__ void __launch_bounds__(256)
     pack_rows_kernel(const T* __restrict__ src, size_t lds, int rows, int cols, T* __restrict__ dst, int ldd, int rows_to) {
@@ -504,6 +515,8 @@ struct DzArgs {
   int ldz, rows, tile0, tiles_n;
 };
 
+// A tile of logits once more, and dz in place of it.  13,568 x 50,304, K = 2,560, bfloat16: 3.1 ms, 1,125 TFLOP/s: the product's 2.7 and the
+// epilogue, 1.4 GB of dz included, of which a CU that has one large tile overlaps nothing with its next.
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) dz_kernel(DzArgs a) {
   PT_STAGES(S)
@@ -567,7 +580,8 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) dz_kernel(DzArg
   }
 }
 
-// out [M, N] (T or float) = scale * A W', or the fp32 slabs of a product cut along K
+// out [M, N] (T or float) = scale * A W', or the fp32 slabs of a product cut along K.  dz of 13,568 x 50,304 in bfloat16, d = 2,560: dh 2.9 ms
+// (1,200 TFLOP/s, and 0.17 for the sum of six slabs), dW 2.8 (1,250): matrix products, near what the library's reach.
 struct OutArgs {
   const void *A, *W, *w_end;  // (see pt_product)
   uint32_t lda, ldw;
@@ -733,6 +747,7 @@ struct Bump {
 };
 
 constexpr int kLogitRows = 16384;  // rows of stored logits at a time
+constexpr int kSumRows = 65536;    // rows at a time where none are: a launch's threads stay below 2^32, the parts' sums at 0.6 GB
 constexpr int kGradRows = 16384;   // rows of dz at a time
 
 int equal_chunk(int T, int most) {  // rows of a chunk: as few chunks as there must be, of about the same size
@@ -807,7 +822,7 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
   Bump ws{(char*)workspace};
   const int parts = (a.V + kPart - 1) / kPart;
   const Operand h = packed(ws, a.hidden, a.T, a.d, a.dtype, false, s), w = packed(ws, a.weight, a.V, a.d, a.dtype, false, s);
-  const int rows = a.top ? equal_chunk(a.T, kLogitRows) : a.T;
+  const int rows = equal_chunk(a.T, a.top ? kLogitRows : kSumRows);
   StatsArgs k;
   float* const part = ws.take<float>((size_t)3 * parts * rows);
   float* const ztgt = ws.take<float>(rows);

@@ -62,7 +62,7 @@ SIZES = [  # T, d, V, type, alternatives
     (1, 64, 100, "bf16", 3), (1, 1, 1, "fp32", 1), (2, 5, 3, "fp16", 3), (3, 37, 77, "fp16", 5), (5, 64, 64, "fp32", 64),
     (7, 32, 65, "fp32", 2), (17, 128, 1000, "bf16", 20), (31, 2560, 300, "bf16", 4), (33, 72, 129, "bf16", 64),
     (64, 768, 4099, "fp16", 0), (65, 96, 515, "fp32", 1), (130, 96, 130, "fp16", 0), (300, 520, 3001, "fp16", 12), (1030, 64, 2049, "bf16", 7),
-    (4200, 64, 777, "fp16", 2),
+    (4200, 64, 777, "fp16", 2), (17000, 64, 200, "bf16", 3), (66000, 64, 70, "fp16", 0),
 ]
 
 
