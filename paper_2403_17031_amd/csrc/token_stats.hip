@@ -53,9 +53,9 @@ struct StatsArgs {
   const float* thr;         // [T] or null: only parts whose maximum is not below their row's are stored
 };
 
-// A tile of logits in the accumulators and what is kept of it.  The epilogue is vector work (a maximum, an exponential and five more
-// instructions an entry) that the matrix cores wait for: 10 us of a tile of 256 x 256, whose product takes 1.7 us a stage, which is
-// why K = 768 runs at 60 % of the rate that K = 2,560 does.  13,568 x 50,304, K = 2,560: 2.6 ms of the call's 2.74.
+// A tile of logits in the accumulators and what is kept of it.  The epilogue is vector work (a maximum, an exponential and seven more
+// instructions an entry) that the matrix cores wait for: 9 us of a tile of 256 x 256, whose product takes 1.7 us a stage, which is
+// why K = 768 runs at two thirds of the rate that K = 2,560 does.  13,568 x 50,304, K = 2,560: 2.6 ms of the call's 2.74.
 template <typename T, typename S>
 __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) stats_kernel(StatsArgs a) {
   PT_STAGES(S)
@@ -98,13 +98,12 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) stats_kernel(St
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float t = fmaxf((acc[j][i][e] - m) * c2, -1e30f);  // (0 times -infinity)
-            float x = __builtin_amdgcn_exp2f(t);
-            if (acc[j][i][e] != acc[j][i][e]) x = acc[j][i][e];      // (the maximum passes over NaN)
+            const float t = (acc[j][i][e] - m) * c2;
+            float x = __builtin_amdgcn_exp2f(t);  // (of NaN, which the maximum passes over, NaN)
             if (!ALL) x = pt_col(j, e, hf) < lim ? x : 0.f;
             s0 += x;
             less += __builtin_amdgcn_fractf(x);
-            s1 = fmaf(x, t, s1);
+            s1 = fmaf(x, fmaxf(t, -1e30f), s1);  // (0 times -infinity)
           }
       } else {  // -infinity alone, or NaN
 #pragma unroll
