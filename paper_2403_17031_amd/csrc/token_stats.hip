@@ -332,7 +332,9 @@ __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
   __shared__ float row_max[16], row_log[16];
   constexpr int G = 256 / R;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = tid % R, g = tid / R, P = a.parts | 1;
-  const int row = blockIdx.x * R + r;
+  const int block = pt_item((a.T + R - 1) / R);  // (neighbours on one XCD: their rows share the lines of the parts' sums)
+  if (block < 0) return;
+  const int row = block * R + r;
   const bool in = row < a.T;
   uint32_t* const pm = (uint32_t*)dyn;
   Stat s = {-INFINITY, -1.f, 0.f};
@@ -391,7 +393,7 @@ __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
   uint32_t* const cand = pm + R * P + wave * finish_words(a.top);
   int *const chosen = (int*)(cand + a.top * kPart), *const sel = chosen + a.top;
   for (int q = wave; q < R; q += 4) {
-    const int t = blockIdx.x * R + q;
+    const int t = block * R + q;
     if (t >= a.T) break;
     if (a.top <= kQuickTop) {
       int *const places = (int*)cand, *const cols = places + kQuickParts + 64;
@@ -440,13 +442,15 @@ __global__ void __launch_bounds__(256) stats_threshold_kernel(const float* __res
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = parts | 1;
   uint32_t* const pm = (uint32_t*)dyn;
+  const int block = pt_item((T + 15) / 16);
+  if (block < 0) return;
   for (int i = tid; i < 16 * parts; i += 256) {
-    const int row = blockIdx.x * 16 + (i & 15);
+    const int row = block * 16 + (i & 15);
     if (row < T) pm[(i & 15) * P + (i >> 4)] = order_key(pmax[(size_t)(i >> 4) * T + row]);
   }
   __syncthreads();
   for (int q = wave; q < 16; q += 4) {
-    const int row = blockIdx.x * 16 + q;
+    const int row = block * 16 + q;
     if (row >= T) break;
     uint32_t largest = 0;
     for (int i = lane; i < parts; i += 64) largest = max(largest, pm[q * P + i]);
@@ -859,7 +863,7 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
       const int big = big_columns(n, a.V, a.dtype), mids = (a.V + 127) / 128;
       if (const int first = sample_tiles(n, a.V, a.d, a.top, a.dtype)) {
         run(PtBig(), 0, first);
-        hipLaunchKernelGGL(stats_threshold_kernel, dim3((n + 15) / 16), dim3(256), 16 * (size_t)(4 * first | 1) * 4, s, k.pmax, n, 4 * first,
+        hipLaunchKernelGGL(stats_threshold_kernel, dim3(pt_grid((n + 15) / 16)), dim3(256), 16 * (size_t)(4 * first | 1) * 4, s, k.pmax, n, 4 * first,
                            a.top, thr);
         k.thr = thr;
         const int then = first + big_columns(n, a.V - 256 * first, a.dtype);
@@ -879,7 +883,7 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
                     a.top ? a.top_logprob + (size_t)t0 * a.top : nullptr};
     auto finish = [&](auto r) {
       constexpr int R = decltype(r)::value;
-      hipLaunchKernelGGL(stats_finish_kernel<R>, dim3((n + R - 1) / R), dim3(256), finish_lds(parts, R, a.top), s, f);
+      hipLaunchKernelGGL(stats_finish_kernel<R>, dim3(pt_grid((n + R - 1) / R)), dim3(256), finish_lds(parts, R, a.top), s, f);
     };
     // rows of a finishing block: many share the lines of the parts' sums, few leave no CU idle
     if (n >= 4096 && finish_lds(parts, 8, a.top) <= 60 * 1024) finish(std::integral_constant<int, 8>{});
