@@ -240,7 +240,8 @@ int rlhf_adamw_step(float *param, const float *grad, float *exp_avg, float *exp_
  * states after its final LayerNorm and its embed_out.  targets: dev int32 [T]; outputs dev float (ids int32), all but the
  * alternatives required.  V at most 262,144.  Products are summed in fp32; logits are not rounded to the inputs' type.
  * Where d is not a multiple of 64 (32 for float) or a row is not whole 16 bytes, a matrix is copied into the workspace
- * first (in the backward call, where V or T is not such a multiple, its last rows are).  Rows do not depend on each other.
+ * first (in the backward call, where V or T is not such a multiple, its last rows are).  Rows do not depend on each other
+ * (but for last bits: how a product is cut depends on T).
  * With top_k = 0 no logit is stored; else there is room for those of 16,384 rows at a time in the workspace. */
 int rlhf_token_stats_workspace_bytes(int32_t T, int32_t d, int32_t V, int64_t ld_hidden, int64_t ld_weight, int32_t dtype,
                                      int32_t top_k, size_t *out);

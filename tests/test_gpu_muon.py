@@ -77,6 +77,21 @@ def test_a_batch_is_its_matrices():
     assert P.orthogonalize(x[:0]).shape == (0, 70, 130)
 
 
+def test_more_elements_than_go_together():
+    """Nine matrices of 33.6 M elements, seven of which fill the workspace: the eighth and ninth share its second filling."""
+    import torch
+    n = 5800
+    x = 1e-3 * torch.randn(9, n, n, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    got = P.orthogonalize(x)
+    for i in (0, 6, 7, 8):
+        assert torch.equal(got[i], P.orthogonalize(x[i]))
+    X = x[8].double() / (x[8].double().norm() + 1e-7)
+    for _ in range(5):
+        A = X @ X.T.contiguous()
+        X = 3.4445 * X + (-4.7750 * A + 2.0315 * (A @ A)) @ X
+    assert float((got[8].double() - X).norm() / X.norm()) <= 4e-3
+
+
 def test_nothing_infinities_and_tiny_values():
     import torch
     x = torch.zeros(4, 70, 90, device="cuda")

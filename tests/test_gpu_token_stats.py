@@ -336,6 +336,32 @@ def test_gradient_over_several_chunks_of_rows():
             assert float((got[n].double() - want).norm() / want.norm()) <= u[dtype] + u[gdtype] + 1e-5, (dtype, gdtype, n)
 
 
+def test_offsets_beyond_32_bits():
+    """8,300 rows of 262,144 entries: more logits, and more entries of dl, than 31 bits count; the first and the last of them.  The
+    gradient's bars are those of the chunks' test."""
+    import torch
+    T, d, V = 8300, 64, 1 << 18
+    h, w, y, th, tw, ty = _inputs(T, d, V, "bf16", 8)
+    some = np.r_[0:5, T - 20:T]
+    s = P.token_stats(th, tw, ty, 0.7, 3)
+    _check({n: x[torch.from_numpy(some).cuda()] for n, x in s.items()}, h[some], w, y[some], 0.7, 3)
+    gl, ge = torch.randn(T, device="cuda"), 0.1 * torch.randn(T, device="cuda")
+    got = P.token_stats_backward(th, tw, ty, s["lse"], s["entropy"], gl, ge, 0.7)
+
+    def dl(rows, cols):
+        logp = th[rows].double() @ tw[cols].double().T / 0.7 - s["lse"][rows, None].double()
+        g = torch.where(ty[rows] >= 0, gl[rows], 0.0).double()[:, None]
+        p = logp.exp()
+        own = ty[rows, None] == torch.arange(V, device="cuda")[cols]
+        return (g * own - p * (g + ge[rows, None].double() * (logp + s["entropy"][rows, None].double()))) / 0.7
+
+    everything = slice(0, None)
+    for have, want in ((got["d_hidden"][-20:], dl(slice(T - 20, T), everything) @ tw.double()),
+                       (got["d_hidden"][:5], dl(slice(0, 5), everything) @ tw.double()),
+                       (got["d_weight"][-64:], dl(everything, slice(V - 64, V)).T @ th.double())):
+        assert float((have.double() - want).norm() / want.norm()) <= 2 * 2.0**-8 + 1e-5
+
+
 def test_gradient_matches_differences_of_the_forward_call():
     """fp32, through the library alone: the loss's change along a direction against the gradient."""
     import torch
