@@ -974,6 +974,7 @@ int rlhf_token_stats(const void* hidden, int64_t ld_hidden, const void* weight, 
   a.weight.p = weight;
   a.targets = targets;
   a.inv_t = 1.0f / temperature;
+  a.inv_lo = (float)(1.0 / (double)temperature - (double)a.inv_t);
   a.logprob = out_logprobs;
   a.entropy = out_entropy;
   a.lse = out_lse;
@@ -1031,6 +1032,7 @@ int rlhf_token_stats_backward(const void* hidden, int64_t ld_hidden, const void*
   a.d_logprob = d_logprobs;
   a.d_entropy = d_entropy;
   a.inv_t = 1.0f / temperature;
+  a.inv_lo = (float)(1.0 / (double)temperature - (double)a.inv_t);
   a.d_hidden = d_hidden;
   a.d_weight = d_weight;
   hipError_t e = hipSuccess;

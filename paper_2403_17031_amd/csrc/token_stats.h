@@ -21,7 +21,7 @@ struct TokenStatsArgs {
   TokenRows hidden, weight;
   const int32_t* targets;
   int T, d, V, dtype, top;
-  float inv_t;
+  float inv_t, inv_lo;  // 1 / temperature in two floats
   float *logprob, *entropy, *lse;
   int32_t* top_ids;
   float* top_logprob;
@@ -33,7 +33,7 @@ struct TokenGradArgs {
   const int32_t* targets;
   const float *lse, *entropy, *d_logprob, *d_entropy;
   int T, d, V, dtype;
-  float inv_t;
+  float inv_t, inv_lo;  // 1 / temperature in two floats
   bool grad_f32;
   void *d_hidden, *d_weight;
 };

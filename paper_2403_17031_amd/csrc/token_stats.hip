@@ -184,7 +184,7 @@ struct FinishArgs {
   const float *pmax, *ps0, *ps1, *ztgt, *logits;
   const int32_t* targets;
   int T, V, parts, ldl, top;
-  float inv_t;
+  float inv_t, inv_lo;  // (inv_lo: what inv_t was rounded by)
   float *logprob, *entropy, *lse;
   int32_t* top_ids;
   float* top_logprob;
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(256) stats_finish_kernel(FinishArgs a) {
     const float ls = log1pf(excess);
     row_max[r] = m;
     row_log[r] = ls;
-    a.lse[row] = m * a.inv_t + ls;
+    a.lse[row] = fmaf(m, a.inv_t, fmaf(fmaxf(m, -1e30f), a.inv_lo, ls));
     a.entropy[row] = ls - s1 / (1.f + excess);
     const int y = a.targets[row];
     a.logprob[row] = y >= 0 && y < a.V ? (a.ztgt[row] - m) * a.inv_t - ls : 0.f;
@@ -513,7 +513,7 @@ struct DzArgs {
   const int32_t* targets;
   const float *lse, *entropy, *g, *e;  // e may be null
   const float* scale;                  // null: 1
-  float inv_t;
+  float inv_t, inv_lo;   // (see FinishArgs)
   void* dz;  // [rows][ldz], zero from T and V on
   int ldz, rows, tile0, tiles_n;
 };
@@ -549,8 +549,9 @@ __global__ void __launch_bounds__(64 * S::waves, pt_waves_eu<S>) dz_kernel(DzArg
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
-        // (a finite log p: 0 times infinity)
-        const float logp = fmaf(acc[j][i][x], a.inv_t, -lse), p = __expf(logp);
+        // (a finite log p: 0 times infinity; the reciprocal's rounding is one sign over a row, which float would show)
+        const float logp = fmaf(acc[j][i][x], a.inv_t, sizeof(T) == 4 ? fmaf(fmaxf(acc[j][i][x], -1e30f), a.inv_lo, -lse) : -lse),
+                    p = __expf(logp);
         acc[j][i][x] = -p * (g + e * (fmaxf(logp, -1e30f) + H));
       }
     const int tcol = y >= 0 ? y - col0 : -1;
@@ -878,7 +879,7 @@ size_t token_stats_plan(const TokenStatsArgs& a, void* workspace, hipStream_t s,
         if (!done && 2 * big < mids) run(PtMid(), 2 * big, mids);
       }
     });
-    FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, a.inv_t,
+    FinishArgs f = {k.pmax, k.ps0, k.ps1, ztgt, logits, k.targets, n, a.V, parts, k.ldl, a.top, a.inv_t, a.inv_lo,
                     a.logprob + t0, a.entropy + t0, a.lse + t0, a.top ? a.top_ids + (size_t)t0 * a.top : nullptr,
                     a.top ? a.top_logprob + (size_t)t0 * a.top : nullptr};
     auto finish = [&](auto r) {
@@ -968,7 +969,7 @@ size_t token_stats_backward_plan(const TokenGradArgs& a, void* workspace, hipStr
     const int n = std::min(rows, a.T - t0);
     const void* const hp = (const char*)h.p + (size_t)t0 * h.ld * esz;
     DzArgs k = {hp, w.p, h.ld, w.ld, n, a.V, whole(a.d, stage), a.targets + t0, a.lse + t0, (a.d_entropy ? a.entropy : a.lse) + t0, a.d_logprob + t0,
-                      a.d_entropy ? a.d_entropy + t0 : nullptr, scaled ? scale : nullptr, a.inv_t, dz, ldz, whole(n, stage), 0, 0};
+                      a.d_entropy ? a.d_entropy + t0 : nullptr, scaled ? scale : nullptr, a.inv_t, a.inv_lo, dz, ldz, whole(n, stage), 0, 0};
     OutArgs oh = {}, ow = {};
     oh.A = dz;
     oh.lda = ldz;
