@@ -322,7 +322,8 @@ __device__ __forceinline__ int bounded_places(const uint32_t* keys, int n, int k
 }
 
 // Block: R rows, 256 / R threads to each for the sums; then a wave per row for the alternatives.  Bound by the latency of its few
-// dependent reads: 13,568 rows of 786 parts with eight alternatives 120 us (the parts' 128 MB would take 26), 1,003 rows 18, one row 9.
+// dependent reads: 13,568 rows of 786 parts with eight alternatives 86 us (the parts' 128 MB would take 26; 120 where neighbours, whose rows
+// share lines, run on different XCDs), 1,003 rows 14, one row 9.
 // LDS: the keys of the rows' part maxima [R][parts | 1] (with alternatives), then of each wave its candidates' [top * 64] and the
 // parts [top], as chosen and by id, or (the quick way) the parts [32] and the keys and ids of what is ranked [64].
 template <int R>
